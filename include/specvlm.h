@@ -48,7 +48,8 @@ typedef enum specvlm_status {
   SPECVLM_ERR_WORKSPACE_TOO_SMALL = -3,
   SPECVLM_ERR_CUDA = -4,              /* a CUDA runtime / driver call failed                   */
   SPECVLM_ERR_TIMEOUT = -5,           /* device-side bounded wait expired (via d_status only)  */
-  SPECVLM_ERR_TOO_LARGE = -6          /* problem exceeds the fixed capacity of a no-allocation call */
+  SPECVLM_ERR_TOO_LARGE = -6,         /* problem exceeds the fixed capacity of a no-allocation call */
+  SPECVLM_ERR_NO_PAGES = -7           /* a page pool has too few free pages (via d_status only)  */
 } specvlm_status;
 
 /*
@@ -358,6 +359,130 @@ int32_t specvlm_accept_tree(const float* target_logits, const int32_t* node_toke
 int32_t specvlm_compact_tree_kv(const specvlm_kv_t* kv, const int32_t* path, const int32_t* accept_len,
                                 int32_t batch, int32_t n_nodes, int32_t* seq_lens_inout, int32_t* d_status,
                                 void* stream);
+
+/* ---------------------------------------------------------------------------------------------
+ * Rotary positions of a call's new tokens, and their append to the cache.  (The paper's models use
+ * rotary positions; the paper has no counterpart of the call.)
+ *
+ * Pair i of a row's first rot_dim channels is turned by the angle 2 pi * position * turns[i], and
+ * scaled by `factor`:
+ *   half layout (interleaved = 0): channels i and i + rot_dim / 2;  interleaved: channels 2 i and 2 i + 1
+ *   (x, y) -> factor * (x cos - y sin, y cos + x sin)
+ * Channels from rot_dim on pass unchanged.  turns[i] is the fraction of a turn that one position makes, as a
+ * 64-bit fixed-point number (2^64 = a whole turn): position * turns modulo a turn is then exact integer
+ * arithmetic, however far the position.  specvlm_rope_turns makes them from frequencies in radians a position,
+ * specvlm_rope_frequencies those of the usual scalings.
+ * With n_axes = 2 or 3 a token has a position on each axis (time, height, width of video tokens): the first
+ * sections[0] pairs take axis 0, the next sections[1] axis 1, the rest axis 2; the sections add up to rot_dim / 2.
+ */
+typedef struct specvlm_rope {
+  const uint64_t* turns;        /* device [rot_dim / 2]                                      */
+  int32_t rot_dim;              /* rotated channels: a multiple of 16, 16 .. head_dim        */
+  int32_t interleaved;
+  int32_t n_axes;               /* 1 .. 3                                                    */
+  int32_t sections[3];          /* pairs of each axis (n_axes > 1)                           */
+  float factor;                 /* scale of rotated channels (1; more for some long contexts) */
+} specvlm_rope_t;
+
+/* Token rows [n_layers][batch][n_new][heads][head_dim] of bf16: strides in elements, multiples of 8; 16-byte aligned. */
+typedef struct specvlm_rows {
+  void* p;                      /* device, NULL: none */
+  int64_t stride_layer, stride_batch, stride_token, stride_head;
+} specvlm_rows_t;
+
+/* Host only: turns[i] = frequency[i] / (2 pi) modulo 1, in units of 2^-64 (n values; finite frequencies). */
+int32_t specvlm_rope_turns(const double* frequencies, int32_t n, uint64_t* turns);
+
+/*
+ * Host only: frequencies f_i = base^(-2 i / rot_dim), i < rot_dim / 2, scaled for contexts `scale` times as long as the
+ * trained one of `context` positions.
+ *   PLAIN    as they are                      LINEAR   f_i / scale
+ *   BASE     with base * scale^(rot_dim / (rot_dim - 2)): the longest wave is stretched by scale, the shortest is left
+ *   RAMP     between the pairs that make `high` and `low` turns within the trained context (rounded outwards to whole
+ *            pairs) a linear blend from f_i to f_i / scale; faster ones stay, slower ones are divided
+ *   BANDS    the same blend linear in the number of turns w_i = context f_i / (2 pi): f_i ((w_i - low) / (high - low)) +
+ *            (f_i / scale) ((high - w_i) / (high - low)) for low <= w_i <= high
+ */
+typedef enum specvlm_rope_scaling {
+  SPECVLM_ROPE_PLAIN = 0,
+  SPECVLM_ROPE_LINEAR = 1,
+  SPECVLM_ROPE_BASE = 2,
+  SPECVLM_ROPE_RAMP = 3,
+  SPECVLM_ROPE_BANDS = 4
+} specvlm_rope_scaling;
+int32_t specvlm_rope_frequencies(int32_t scaling, int32_t rot_dim, double base, double scale, double context, double low,
+                                 double high, double* frequencies);
+
+/*
+ * Rotates n_new tokens' queries and keys of every sequence and appends keys and values to the cache.  Token t of
+ * sequence b goes to cache position start_b + t of every layer and KV head and has positions[a][b][t] on axis a.
+ *   kv           host struct of the cache to extend (kv->seq_lens is ignored, see seq_lens_inout)
+ *   q, q_out     rows of n_q_heads heads, both or neither (p NULL); q_out may be q itself, else they do not overlap
+ *   new_k, new_v rows of kv->n_kv_heads heads; they do not overlap the cache or q_out
+ *   positions_or_null  device int32 [n_axes][batch][n_new] (any sign); NULL: start_b + t on every axis
+ *   new_lens_or_null   device int32 [batch], 0 .. n_new: sequence b has only that many new tokens, the rows behind them are
+ *                padding: not rotated, not appended, q_out left as it was.  NULL: n_new each
+ *   seq_lens_inout     device int32 [batch].  counted = 0: lengths before the append, start_b = seq_lens[b]; the new tokens
+ *                are added to them at the end.  counted != 0: lengths that include the new tokens already (a program that
+ *                calls layer by layer lets the first layer's call count them), start_b = seq_lens[b] - new; not written
+ * A sequence whose length, or number of new tokens, is out of range (start_b < 0, or more than kv->max_seq_len tokens) is
+ * left alone, its rows of q_out too, and SPECVLM_ERR_INVALID_ARG is stored to d_status.  A token whose block-table entry
+ * is outside [0, n_blocks) is not appended (its query is rotated), and reported the same way.
+ * The rotation runs in fp32 and is rounded once.
+ */
+int32_t specvlm_rope_append_kv(const specvlm_kv_t* kv, const specvlm_rope_t* rope, const specvlm_rows_t* q,
+                               const specvlm_rows_t* q_out, const specvlm_rows_t* new_k, const specvlm_rows_t* new_v,
+                               int32_t batch, int32_t n_new, int32_t n_q_heads, const int32_t* positions_or_null,
+                               const int32_t* new_lens_or_null, int32_t* seq_lens_inout, int32_t counted,
+                               int32_t* d_status, void* stream);
+
+/* ---------------------------------------------------------------------------------------------
+ * Pages of a paged cache.  (The paper has no counterpart.)  The state of the pool is one count a page: ref_count[n] =
+ * how many block-table rows hold page n, 0 = free.  A table entry outside [0, n_blocks) is unmapped; these calls write -1.
+ * A call covers all layers: kv describes the whole pool.  Several rows may hold a page (branches that share what came
+ * before them); a row that is written to has the page to itself.  All of these calls are deterministic: free pages are
+ * taken lowest first, by sequence and then position.  batch <= 1024.
+ *   ref_count_inout     device int32 [n_blocks]; at the start of a program zeros, with every table entry -1
+ *   block_table_inout   device int32 [batch][kv->max_blocks], takes kv->block_table's place
+ *   ws                  device scratch, specvlm_pages_workspace_bytes(kv, batch)
+ * The counts and the tables have to agree: every table whose rows hold pages of the pool takes part in its compaction.
+ *
+ * specvlm_reserve_pages makes the next positions of every sequence writable: kv->seq_lens[b] .. + new - 1, with new =
+ * new_lens[b] or n_new.  Of the pages that these fall on, an unmapped one is taken from the free ones; one that other rows
+ * hold too is replaced by a fresh one, into which the rows that the sequence has on it already are copied (K and V, all
+ * layers and heads), except that of several sequences of the call that go on in one and the same page the last keeps it
+ * if nobody else holds it.  Pages replaced here are not handed out in the same call.  All or nothing: with too few free pages nothing changes, and SPECVLM_ERR_NO_PAGES is stored to
+ * d_status.  A sequence without room (more than kv->max_seq_len tokens), or with a length or number of new tokens out of
+ * range, gets nothing, and SPECVLM_ERR_INVALID_ARG is stored; the others get theirs.
+ *
+ * specvlm_release_pages gives back the pages that hold no row that is still needed: those wholly behind the sequence's
+ * end, and those whose rows are all older than the last `window` tokens and not among the first n_sinks (1 <= window;
+ * INT32_MAX: no window).  After the attention of a step a window of window_attn's size is enough; while n_q tokens that
+ * are counted in seq_lens have yet to attend, window + n_q - 1 is.  A sequence of length 0 gives back everything.
+ *
+ * specvlm_fork_pages replaces a batch of sequences by another: row i of block_table_out and seq_lens_out goes on from
+ * sequence parents[i] of kv (-1: empty).  Sequences that nobody goes on from give their pages back, and those with several
+ * branches share theirs; no row is copied (specvlm_reserve_pages does that when a branch is written to).  Pages behind a
+ * sequence's end are given back.  kv's table and lengths are not written, and hold no pages afterwards.
+ *   parents          device int32 [batch_out], batch_out <= 1024
+ *   block_table_out  device int32 [batch_out][kv->max_blocks], does not overlap kv->block_table
+ *   seq_lens_out     device int32 [batch_out], does not overlap kv->seq_lens
+ *
+ * specvlm_compact_pages moves the used pages to the front of the pool: with n used pages, the i-th used page from page n
+ * on moves into the i-th free page below n (K and V, all layers and heads), and counts and table follow.
+ *   n_used_or_null   device int32 out: the number of used pages
+ */
+size_t specvlm_pages_workspace_bytes(const specvlm_kv_t* kv, int32_t batch);
+int32_t specvlm_reserve_pages(const specvlm_kv_t* kv, int32_t* block_table_inout, int32_t* ref_count_inout, int32_t batch,
+                              int32_t n_new, const int32_t* new_lens_or_null, void* ws, size_t ws_bytes,
+                              int32_t* d_status, void* stream);
+int32_t specvlm_release_pages(const specvlm_kv_t* kv, int32_t* block_table_inout, int32_t* ref_count_inout, int32_t batch,
+                              int32_t window, int32_t n_sinks, int32_t* d_status, void* stream);
+int32_t specvlm_fork_pages(const specvlm_kv_t* kv, int32_t* ref_count_inout, int32_t batch, const int32_t* parents,
+                           int32_t batch_out, int32_t* block_table_out, int32_t* seq_lens_out, int32_t* d_status,
+                           void* stream);
+int32_t specvlm_compact_pages(const specvlm_kv_t* kv, int32_t* block_table_inout, int32_t* ref_count_inout, int32_t batch,
+                              int32_t* n_used_or_null, void* ws, size_t ws_bytes, int32_t* d_status, void* stream);
 
 /* ---------------------------------------------------------------------------------------------
  * specvlm_accept without any caller-provided scratch.  (The paper has no counterpart: this is a

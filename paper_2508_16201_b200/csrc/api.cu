@@ -17,6 +17,7 @@ extern "C" const char* specvlm_status_string(int32_t status) {
     case SPECVLM_ERR_CUDA: return "CUDA call failed";
     case SPECVLM_ERR_TIMEOUT: return "device-side wait timed out";
     case SPECVLM_ERR_TOO_LARGE: return "problem exceeds the built-in scratch of a no-allocation call";
+    case SPECVLM_ERR_NO_PAGES: return "too few free pages";
     default: return "unknown status";
   }
 }

@@ -3,7 +3,8 @@
 // and 0.1 us on each tensor's address, of 5 to 8 us that a short call takes on the host.
 //
 // Every function takes the C arguments in order without the stream, which is the current one of the current device:
-//   KvStruct    its address (int)       device pointer   a tensor (its data_ptr()) or None; a number is refused
+//   KvStruct, RopeStruct   the address (int)   device pointer   a tensor (its data_ptr()) or None; a number is refused
+//   token rows  a tensor of five dimensions with a unit last stride, or None
 //   host array  any sequence of integers; integers are taken modulo 2^32, as ctypes takes them
 // and returns the status.  The interpreter lock is released during the call.
 #define PY_SSIZE_T_CLEAN
@@ -21,6 +22,7 @@ namespace {
 PyObject* g_get_device = nullptr;      // torch._C._cuda_getDevice
 PyObject* g_get_raw_stream = nullptr;  // torch._C._cuda_getCurrentRawStream
 PyObject* g_data_ptr = nullptr;        // "data_ptr"
+PyObject* g_stride = nullptr;          // "stride"
 
 struct AnyPtr {
   void* p;
@@ -28,15 +30,18 @@ struct AnyPtr {
 };
 
 // One class per kind of argument: set() converts, get() is what the C function takes.
-struct Kv {
+template <typename T>
+struct Struct {
   static constexpr int kArgs = 1;
-  const specvlm_kv_t* v = nullptr;
+  const T* v = nullptr;
   bool set(PyObject* o) {
-    v = static_cast<const specvlm_kv_t*>(PyLong_AsVoidPtr(o));
+    v = static_cast<const T*>(PyLong_AsVoidPtr(o));
     return !PyErr_Occurred();
   }
-  const specvlm_kv_t* get() const { return v; }
+  const T* get() const { return v; }
 };
+using Kv = Struct<specvlm_kv_t>;
+using Rope = Struct<specvlm_rope_t>;
 struct Ptr {
   static constexpr int kArgs = 1;
   void* v = nullptr;
@@ -49,6 +54,35 @@ struct Ptr {
     return !PyErr_Occurred();
   }
   AnyPtr get() const { return {v}; }
+};
+struct Rows {
+  static constexpr int kArgs = 1;
+  specvlm_rows_t v = {};
+  bool set(PyObject* o) {
+    Ptr p;
+    if (!p.set(o)) return false;
+    v.p = p.v;
+    if (o == Py_None) return true;
+    PyObject* const s = PyObject_CallMethodNoArgs(o, g_stride);
+    if (!s) return false;
+    long long x[5] = {0, 0, 0, 0, 0};
+    bool ok = PyTuple_Check(s) && PyTuple_GET_SIZE(s) == 5;
+    for (int i = 0; ok && i < 5; ++i) {
+      x[i] = PyLong_AsLongLong(PyTuple_GET_ITEM(s, i));
+      ok = !PyErr_Occurred();
+    }
+    Py_DECREF(s);
+    if (ok && x[4] == 1) {
+      v.stride_layer = x[0];
+      v.stride_batch = x[1];
+      v.stride_token = x[2];
+      v.stride_head = x[3];
+      return true;
+    }
+    if (!PyErr_Occurred()) PyErr_SetString(PyExc_ValueError, "rows of five dimensions with a unit last stride are expected");
+    return false;
+  }
+  const specvlm_rows_t* get() const { return &v; }
 };
 // An integer, or what stands for one (__index__: numpy's integers, tensors of one integer); a float is none.
 bool to_int(PyObject* o, unsigned long long& v) {
@@ -199,6 +233,11 @@ PyMethodDef g_methods[] = {
     SPECVLM_ENTRY(append_kv, Kv, Ptr, Ptr, I32, I32, Ptr, Ptr),
     SPECVLM_ENTRY(rollback_kv, Ptr, Ptr, I32, I32, Ptr),
     SPECVLM_ENTRY(compact_tree_kv, Kv, Ptr, Ptr, I32, I32, Ptr, Ptr),
+    SPECVLM_ENTRY(rope_append_kv, Kv, Rope, Rows, Rows, Rows, Rows, I32, I32, I32, Ptr, Ptr, Ptr, I32, Ptr),
+    SPECVLM_ENTRY(reserve_pages, Kv, Ptr, Ptr, I32, I32, Ptr, Ptr, Size, Ptr),
+    SPECVLM_ENTRY(release_pages, Kv, Ptr, Ptr, I32, I32, I32, Ptr),
+    SPECVLM_ENTRY(fork_pages, Kv, Ptr, I32, Ptr, I32, Ptr, Ptr, Ptr),
+    SPECVLM_ENTRY(compact_pages, Kv, Ptr, Ptr, I32, Ptr, Ptr, Size, Ptr),
     {nullptr, nullptr, 0, nullptr}};
 
 PyModuleDef g_module = {PyModuleDef_HEAD_INIT, "_binding", nullptr, -1, g_methods, nullptr, nullptr, nullptr, nullptr};
@@ -207,5 +246,6 @@ PyModuleDef g_module = {PyModuleDef_HEAD_INIT, "_binding", nullptr, -1, g_method
 
 PyMODINIT_FUNC PyInit__binding() {
   g_data_ptr = PyUnicode_InternFromString("data_ptr");
-  return g_data_ptr ? PyModule_Create(&g_module) : nullptr;
+  g_stride = PyUnicode_InternFromString("stride");
+  return g_data_ptr && g_stride ? PyModule_Create(&g_module) : nullptr;
 }

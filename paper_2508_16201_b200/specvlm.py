@@ -23,6 +23,7 @@ ERR_WORKSPACE_TOO_SMALL = -3
 ERR_CUDA = -4
 ERR_TIMEOUT = -5
 ERR_TOO_LARGE = -6
+ERR_NO_PAGES = -7
 
 
 class SpecvlmError(RuntimeError):
@@ -44,6 +45,18 @@ class KvStruct(ctypes.Structure):
     ]
 
 
+class RopeStruct(ctypes.Structure):
+    """Mirror of specvlm_rope_t."""
+    _fields_ = [("turns", c_void_p), ("rot_dim", c_int32), ("interleaved", c_int32), ("n_axes", c_int32),
+                ("sections", c_int32 * 3), ("factor", c_float)]
+
+
+class RowsStruct(ctypes.Structure):
+    """Mirror of specvlm_rows_t."""
+    _fields_ = [("p", c_void_p), ("stride_layer", c_int64), ("stride_batch", c_int64), ("stride_token", c_int64),
+                ("stride_head", c_int64)]
+
+
 _lib = None
 
 EXPORTS = [
@@ -55,7 +68,10 @@ EXPORTS = [
     "specvlm_accept_workspace_bytes", "specvlm_accept", "specvlm_accept_noalloc",
     "specvlm_append_kv", "specvlm_rollback_kv",
     "specvlm_verify_tree_workspace_bytes", "specvlm_verify_tree_attn", "specvlm_accept_tree",
-    "specvlm_compact_tree_kv", "specvlm_debug_poison_shared_memory", "specvlm_debug_wait_timeout",
+    "specvlm_compact_tree_kv",
+    "specvlm_rope_turns", "specvlm_rope_frequencies", "specvlm_rope_append_kv",
+    "specvlm_pages_workspace_bytes", "specvlm_reserve_pages", "specvlm_release_pages", "specvlm_fork_pages",
+    "specvlm_compact_pages", "specvlm_debug_poison_shared_memory", "specvlm_debug_wait_timeout",
     "specvlm_debug_set_attn_splits", "specvlm_debug_window_parts", "specvlm_debug_attn_merge",
     "specvlm_debug_attn_give_up",
 ]
@@ -126,6 +142,25 @@ def lib():
         L.specvlm_append_kv.argtypes = [kvp, c_void_p, c_void_p, c_int32, c_int32, c_void_p, c_void_p, c_void_p]
         L.specvlm_rollback_kv.restype = c_int32
         L.specvlm_rollback_kv.argtypes = [c_void_p, c_void_p, c_int32, c_int32, c_void_p, c_void_p]
+        rowsp = POINTER(RowsStruct)
+        L.specvlm_rope_turns.restype = c_int32
+        L.specvlm_rope_turns.argtypes = [POINTER(ctypes.c_double), c_int32, POINTER(ctypes.c_uint64)]
+        L.specvlm_rope_frequencies.restype = c_int32
+        L.specvlm_rope_frequencies.argtypes = [c_int32, c_int32] + [ctypes.c_double] * 5 + [POINTER(ctypes.c_double)]
+        L.specvlm_rope_append_kv.restype = c_int32
+        L.specvlm_rope_append_kv.argtypes = [kvp, POINTER(RopeStruct), rowsp, rowsp, rowsp, rowsp, c_int32, c_int32, c_int32,
+                                             c_void_p, c_void_p, c_void_p, c_int32, c_void_p, c_void_p]
+        L.specvlm_pages_workspace_bytes.restype = c_size_t
+        L.specvlm_pages_workspace_bytes.argtypes = [kvp, c_int32]
+        L.specvlm_reserve_pages.restype = c_int32
+        L.specvlm_reserve_pages.argtypes = [kvp, c_void_p, c_void_p, c_int32, c_int32, c_void_p, c_void_p, c_size_t, c_void_p,
+                                            c_void_p]
+        L.specvlm_release_pages.restype = c_int32
+        L.specvlm_release_pages.argtypes = [kvp, c_void_p, c_void_p, c_int32, c_int32, c_int32, c_void_p, c_void_p]
+        L.specvlm_fork_pages.restype = c_int32
+        L.specvlm_fork_pages.argtypes = [kvp, c_void_p, c_int32, c_void_p, c_int32, c_void_p, c_void_p, c_void_p, c_void_p]
+        L.specvlm_compact_pages.restype = c_int32
+        L.specvlm_compact_pages.argtypes = [kvp, c_void_p, c_void_p, c_int32, c_void_p, c_void_p, c_size_t, c_void_p, c_void_p]
         L.specvlm_gather_kv.restype = c_int32
         L.specvlm_gather_kv.argtypes = [kvp, c_void_p, i32p, i32p, i32p, i32p, c_int32, kvp, c_void_p,
                                         c_void_p]
@@ -433,6 +468,143 @@ def rollback_kv(seq_lens: torch.Tensor, accept_len: torch.Tensor, gamma: int,
     rc = native().rollback_kv(seq_lens, accept_len, seq_lens.numel(), int(gamma), d_status)
     if rc:
         _check(rc, "specvlm_rollback_kv")
+
+
+# ---------------------------------------------------------------------------------- rotary positions
+ROPE_PLAIN, ROPE_LINEAR, ROPE_BASE, ROPE_RAMP, ROPE_BANDS = 0, 1, 2, 3, 4
+
+
+def rope_frequencies(rot_dim: int, base: float = 10000.0, scaling: int = ROPE_PLAIN, scale: float = 1.0, context: float = 0.0,
+                     low: float = 1.0, high: float = 32.0) -> torch.Tensor:
+    """Frequencies in radians a position, float64 [rot_dim / 2] on the host, scaled for contexts ``scale`` times as long as
+    the trained one of ``context`` positions (ROPE_*)."""
+    f = (ctypes.c_double * max(1, rot_dim // 2))()
+    _check(lib().specvlm_rope_frequencies(int(scaling), int(rot_dim), float(base), float(scale), float(context), float(low),
+                                          float(high), f), "specvlm_rope_frequencies")
+    return torch.tensor(list(f), dtype=torch.float64)
+
+
+class Rope:
+    """A rotation: its frequencies (radians a position, float64, one a pair of channels) as fractions of a turn in device
+    memory, plus the specvlm_rope_t descriptor.
+
+    ``interleaved``: channels 2 i and 2 i + 1 make a pair, else i and i + rot_dim / 2.  ``sections``: pairs of each position
+    axis (two or three), None for one axis.  ``factor`` scales the rotated channels.
+    """
+
+    def __init__(self, frequencies: torch.Tensor, interleaved: bool = False, factor: float = 1.0, sections=None,
+                 device: str | torch.device | None = None):
+        f = torch.as_tensor(frequencies)
+        if device is None:
+            device = f.device if f.is_cuda else torch.device("cuda")
+        n = f.numel()
+        turns = (ctypes.c_uint64 * max(1, n))()
+        _check(lib().specvlm_rope_turns((ctypes.c_double * max(1, n))(*f.double().flatten().tolist()), n, turns), "specvlm_rope_turns")
+        self.turns = torch.frombuffer(turns, dtype=torch.int64).to(device)
+        s = RopeStruct()
+        s.turns, s.rot_dim, s.interleaved, s.factor = self.turns.data_ptr(), 2 * n, 1 if interleaved else 0, float(factor)
+        sections = [int(x) for x in sections] if sections is not None else []
+        s.n_axes = len(sections) or 1
+        for a, x in enumerate(sections[:3]):
+            s.sections[a] = x
+        self.struct = s
+
+    @property
+    def n_axes(self):
+        return self.struct.n_axes
+
+
+def rope_append_kv(kv: KvCache, rope: Rope, q: torch.Tensor | None, new_k: torch.Tensor, new_v: torch.Tensor,
+                   q_out: torch.Tensor | None = None, positions: torch.Tensor | None = None,
+                   new_lens: torch.Tensor | None = None, counted: bool = False,
+                   d_status: torch.Tensor | None = None) -> torch.Tensor | None:
+    """q: bf16 [n_layers][batch][n_new][n_q_heads][head_dim] (None: keys only), new_k / new_v the same with the KV heads, all
+    of any strides with a unit channel stride; returns the rotated queries.  kv.seq_lens is updated unless ``counted``, which
+    says that it includes the new tokens already.  positions: int32 [n_axes][batch][n_new]."""
+    L, B, n, H, D = new_k.shape
+    assert new_k.dtype == torch.bfloat16 and new_v.dtype == torch.bfloat16 and new_v.shape == new_k.shape
+    assert L == kv.n_layers and H == kv.n_kv_heads and D == kv.head_dim
+    n_q_heads = 0
+    if q is not None:
+        n_q_heads = q.shape[3]
+        assert q.dtype == torch.bfloat16 and q.shape == (L, B, n, n_q_heads, D)
+        if q_out is None:
+            q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+        assert q_out.dtype == torch.bfloat16 and q_out.shape == q.shape
+    if positions is not None:
+        assert positions.dtype == torch.int32 and positions.is_contiguous()
+        assert positions.numel() == rope.struct.n_axes * B * n
+    if new_lens is not None:
+        assert new_lens.dtype == torch.int32 and new_lens.is_contiguous() and new_lens.numel() == B
+    rc = native().rope_append_kv(addressof(kv.struct), addressof(rope.struct), q, q_out, new_k, new_v, B, n, n_q_heads, positions,
+                                 new_lens, kv.seq_lens, 1 if counted else 0, d_status)
+    if rc:
+        _check(rc, "specvlm_rope_append_kv")
+    return q_out
+
+
+# ---------------------------------------------------------------------------------- pages
+def pages_workspace_bytes(kv: KvCache, batch: int) -> int:
+    return int(lib().specvlm_pages_workspace_bytes(byref(kv.struct), batch))
+
+
+def _pages(kv: KvCache, ref_count: torch.Tensor) -> int:
+    """Checks what the calls on pages share; returns the batch."""
+    assert kv.block_table is not None, "a cache without a block table has no pages"
+    assert ref_count.dtype == torch.int32 and ref_count.is_contiguous() and ref_count.numel() == kv.k.shape[1]
+    assert kv.seq_lens.numel() >= kv.block_table.shape[0]
+    return kv.block_table.shape[0]
+
+
+def reserve_pages(kv: KvCache, ref_count: torch.Tensor, n_new: int = 0, new_lens: torch.Tensor | None = None,
+                  ws: torch.Tensor | None = None, d_status: torch.Tensor | None = None) -> None:
+    """Makes the next n_new (or new_lens[b]) positions of every sequence writable; kv.block_table and ref_count are updated."""
+    B = _pages(kv, ref_count)
+    if new_lens is not None:
+        assert new_lens.dtype == torch.int32 and new_lens.is_contiguous() and new_lens.numel() == B
+    if ws is None:
+        ws = _ws(pages_workspace_bytes(kv, B), ref_count.device)
+    rc = native().reserve_pages(addressof(kv.struct), kv.block_table, ref_count, B, n_new, new_lens, ws, ws.numel(), d_status)
+    if rc:
+        _check(rc, "specvlm_reserve_pages")
+
+
+def release_pages(kv: KvCache, ref_count: torch.Tensor, window: int | None = None, n_sinks: int = 0,
+                  d_status: torch.Tensor | None = None) -> None:
+    """Gives back the pages without a row that is still needed; kv.block_table and ref_count are updated."""
+    B = _pages(kv, ref_count)
+    rc = native().release_pages(addressof(kv.struct), kv.block_table, ref_count, B, 0x7fffffff if window is None else window,
+                                n_sinks, d_status)
+    if rc:
+        _check(rc, "specvlm_release_pages")
+
+
+def fork_pages(kv: KvCache, ref_count: torch.Tensor, parents: torch.Tensor, block_table_out: torch.Tensor,
+               seq_lens_out: torch.Tensor, d_status: torch.Tensor | None = None) -> None:
+    """Row i of block_table_out / seq_lens_out goes on from sequence parents[i] of kv (-1: empty), whose own table and lengths
+    hold no pages afterwards."""
+    B = _pages(kv, ref_count)
+    n = parents.numel()
+    assert parents.dtype == torch.int32 and parents.is_contiguous()
+    assert block_table_out.dtype == torch.int32 and block_table_out.is_contiguous()
+    assert tuple(block_table_out.shape) == (n, kv.block_table.shape[1])
+    assert seq_lens_out.dtype == torch.int32 and seq_lens_out.is_contiguous() and seq_lens_out.numel() == n
+    rc = native().fork_pages(addressof(kv.struct), ref_count, B, parents, n, block_table_out, seq_lens_out, d_status)
+    if rc:
+        _check(rc, "specvlm_fork_pages")
+
+
+def compact_pages(kv: KvCache, ref_count: torch.Tensor, n_used: torch.Tensor | None = None, ws: torch.Tensor | None = None,
+                  d_status: torch.Tensor | None = None) -> None:
+    """Moves the used pages to the front of the pool; kv's rows, kv.block_table and ref_count are updated."""
+    B = _pages(kv, ref_count)
+    if n_used is not None:
+        assert n_used.dtype == torch.int32 and n_used.numel() >= 1
+    if ws is None:
+        ws = _ws(pages_workspace_bytes(kv, B), ref_count.device)
+    rc = native().compact_pages(addressof(kv.struct), kv.block_table, ref_count, B, n_used, ws, ws.numel(), d_status)
+    if rc:
+        _check(rc, "specvlm_compact_pages")
 
 
 # ---------------------------------------------------------------------------------- tree drafting
