@@ -361,6 +361,27 @@ int32_t specvlm_compact_tree_kv(const specvlm_kv_t* kv, const int32_t* path, con
                                 void* stream);
 
 /* ---------------------------------------------------------------------------------------------
+ * Attention with a sliding window and sinks (the paper has no counterpart: its caches are pruned by importance; a cache
+ * can also be pruned by age).  As specvlm_draft_decode_attn (n_q = 1) and specvlm_verify_attn, but query t, at position
+ * p = seq_len - n_q + t, sees the keys j <= p with j > p - window or j < n_sinks.
+ *   window      >= 1: a token sees itself and window - 1 before it; n_sinks >= 0
+ *   q, out      device bf16 [n_layers][batch][n_q][n_q_heads][head_dim], 1 <= n_q <= 9
+ *   lse_or_null device fp32 [n_layers][batch][n_q][n_q_heads]
+ *   ws          device scratch, specvlm_window_attn_workspace_bytes(kv, batch, n_q_heads, n_q, window, n_sinks)
+ * Keys and values that no query of the call sees are never used, whatever their rows hold; pages that hold no other rows need
+ * not be mapped (specvlm_release_pages).  Rows that some query sees hold finite values.  A block-table entry outside
+ * [0, n_blocks) that is needed stands for rows of zeros, and SPECVLM_ERR_INVALID_ARG is stored to d_status.
+ * A query that sees no key (seq_len < n_q) gives zeros and an lse of -inf.
+ * Supported: head_dim 64/128; group = n_q_heads/n_kv_heads in 1..16 with group * n_q <= 128; batch <= 127 when
+ * group * n_q > 16.  Errors and d_status otherwise as for specvlm_verify_attn.
+ */
+size_t specvlm_window_attn_workspace_bytes(const specvlm_kv_t* kv, int32_t batch, int32_t n_q_heads, int32_t n_q,
+                                           int32_t window, int32_t n_sinks);
+int32_t specvlm_window_attn(const specvlm_kv_t* kv, const void* q, int32_t batch, int32_t n_q_heads, int32_t n_q,
+                            int32_t window, int32_t n_sinks, float sm_scale, void* out, float* lse_or_null, void* ws,
+                            size_t ws_bytes, int32_t* d_status, void* stream);
+
+/* ---------------------------------------------------------------------------------------------
  * Rotary positions of a call's new tokens, and their append to the cache.  (The paper's models use
  * rotary positions; the paper has no counterpart of the call.)
  *

@@ -55,8 +55,11 @@ struct Rows16 {
   }
 
   // tile0: position of the tile's first token; vt: the V tile (generic address); cw: this warp's 16-token slice
-  __device__ __forceinline__ void tile(uint32_t k_base, uint32_t v_base, uint8_t* vt, int tile0, int kv_len, float scale_log2,
+  template <bool WIN, typename P>
+  __device__ __forceinline__ void tile(const P& p, uint32_t k_base, uint32_t v_base, uint8_t* vt, int tile0, const KeyView& view,
                                        int cw, int lane) {
+    const int kv_len = view.len;
+    const float scale_log2 = p.scale_log2;
     const int col = (lane & 3) * 2;
     // per-lane ldmatrix row/chunk selectors
     const int mi = lane >> 3, r8 = lane & 7;
@@ -64,6 +67,20 @@ struct Rows16 {
     const int v_tok = cw * 16 + (mi & 1) * 8 + r8, v_chunk = mi >> 1;   // V: transposed
     const int tb = tile0 + cw * 16;                                      // first token of this warp's slice
     if (tb >= kv_len) return;
+    // positions that no query sees, between the sinks and the window, hold whatever the page holds, as those past the end do
+    const bool hidden = WIN && tb < view.lo && tb + 16 > p.n_sinks;
+    if (hidden) {
+      if (tb >= p.n_sinks && tb + 16 <= view.lo) return;
+      const int first = (p.n_sinks > tb ? p.n_sinks : tb) - tile0, last = (view.lo < tb + 16 ? view.lo : tb + 16) - tile0;
+      for (int t = first + (lane >> 3); t < last; t += 4) {
+#pragma unroll
+        for (int h = 0; h < D / 64; ++h)
+          *reinterpret_cast<uint4*>(vt + h * (kTileTokens * 128) + t * 128 + (lane & 7) * 16) =
+              make_uint4(0, 0, 0, 0);
+      }
+      fence_proxy_async();
+      __syncwarp();
+    }
     if (tb + 16 > kv_len) {
       // rows past the end of the sequence hold whatever the page held: clear V there so that
       // a zero probability times a stale non-finite value cannot reach the accumulator
@@ -95,7 +112,8 @@ struct Rows16 {
       for (int e = 0; e < 4; ++e) {
         const int tok = tb + nt * 8 + col + (e & 1);
         const int lim = (e < 2) ? lim0 : lim1;
-        const float v = tok < lim ? sc[nt][e] * scale_log2 : -INFINITY;
+        const bool seen = tok < lim && (!WIN || tok >= lim - p.window || tok < p.n_sinks);
+        const float v = seen ? sc[nt][e] * scale_log2 : -INFINITY;
         sc[nt][e] = v;
         if (e < 2) mx0 = fmaxf(mx0, v); else mx1 = fmaxf(mx1, v);
       }
@@ -244,15 +262,16 @@ __device__ __forceinline__ void await_copies(uint32_t bar_full, volatile int* fl
 // work through one after the other at 0.35 us each.
 //
 // The consumer warps of an item, or of a cluster's CTA.
-template <int D, int STAGES, int NG, bool SPLIT>
+template <int D, int STAGES, int NG, bool SPLIT, bool WIN>
 __device__ __forceinline__ void rows16_consume(const AttnParams& p, uint8_t* smem, uint32_t base, volatile int* abort_flag,
-                                               int kv_len, int n_my, int rank, int n_cta) {
+                                               const KeyView& view, int n_my, int rank, int n_cta) {
   constexpr int TILE_BYTES = kTileTokens * D * 2, STAGE_BYTES = 2 * TILE_BYTES;
   constexpr int OPITCH = Rows16<D>::OPITCH;
   const uint32_t bar_full = base + STAGES * STAGE_BYTES, bar_empty = bar_full + 8 * STAGES;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int g = blockIdx.y, lb = blockIdx.z;
-  const bool spec = p.block_table == nullptr;
+  const bool spec = !WIN && p.block_table == nullptr;
+  const int kv_len = view.len;
   const int n_all = (kv_len + kTileTokens - 1) / kTileTokens;
 
   if (n_all == 0) {
@@ -269,6 +288,7 @@ __device__ __forceinline__ void rows16_consume(const AttnParams& p, uint8_t* sme
   }
   const int cw = warp & 3, grp = warp >> 2;                           // token slice, consumer group
   Rows16<D> st;
+  // (positions of the newest keys are as far apart as the keys)
   st.start(p, p.n_q, p.rows, lb, g, kv_len, lane);
   bool alive = true;
   // a CTA without a tile of its own: the one asked for before the length was known lands where the merge buffer will be
@@ -280,8 +300,8 @@ __device__ __forceinline__ void rows16_consume(const AttnParams& p, uint8_t* sme
       break;
     }
     const uint32_t k_base = base + s * STAGE_BYTES;
-    st.tile(k_base, k_base + TILE_BYTES, smem + s * STAGE_BYTES + TILE_BYTES, (i * n_cta + rank) * kTileTokens, kv_len,
-            p.scale_log2, cw, lane);
+    st.template tile<WIN>(p, k_base, k_base + TILE_BYTES, smem + s * STAGE_BYTES + TILE_BYTES, (i * n_cta + rank) * kTileTokens, view,
+                          cw, lane);
     __syncwarp();
     if (lane == 0) mbar_arrive(bar_empty + 8 * s);
   }
@@ -378,7 +398,8 @@ __device__ __forceinline__ void rows16_consume(const AttnParams& p, uint8_t* sme
 constexpr int kSoloTiles = 4, kSoloTilesPair = 6;
 // (CTAs per SM are as many as the ring allows; without that the compiler held d = 64 to 96 registers and spilled: 6 layers of
 // 800 tokens, 24 items, 4.4 -> 4.2 us, 112 items of d = 128 and 755 tokens 9.83 -> 9.65)
-template <int D, int STAGES, int NG, bool SPLIT>
+// WIN: queries see a window and sinks (KeyView); the first tile is not known before the length then.
+template <int D, int STAGES, int NG, bool SPLIT, bool WIN = false>
 __global__ void __launch_bounds__(32 * (4 * NG + 1), NG == 2 ? 1 : D == 64 ? 4 : 2)
 attn_rows16_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v,
                    const AttnParams p) {
@@ -423,7 +444,7 @@ attn_rows16_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_consta
   // The first tile of a contiguous cache sits at a known place whatever the sequence's
   // length (rows past the cache's end are zero-filled by the copy): the producer asks for it
   // before the length has even been read, which takes a global-memory round trip off the start.
-  const bool spec = p.block_table == nullptr;
+  const bool spec = !WIN && p.block_table == nullptr;
   if (spec && tid == 32 * 4 * NG) {
     const uint64_t policy = l2_policy_evict_first();
     mbar_arrive_expect_tx(bar_full, STAGE_BYTES);
@@ -434,8 +455,8 @@ attn_rows16_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_consta
     }
   }
 
-  const int kv_len = clamp_len(p.seq_lens[b], p.max_seq_len);
-  const int n_all = (kv_len + kTileTokens - 1) / kTileTokens;
+  const KeyView view = key_view<WIN>(p, p.n_q, b);
+  const int n_all = (view.len + kTileTokens - 1) / kTileTokens;
   const bool solo = SPLIT && n_all <= (n_cta == 2 ? kSoloTilesPair : kSoloTiles);
   const int n_split = SPLIT ? (n_all + n_cta - 1 - rank) / n_cta : n_all;
   const int n_my = !solo ? n_split : rank == 0 ? n_all : 0;
@@ -458,10 +479,11 @@ attn_rows16_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_consta
         const int s = i % STAGES;
         if (i >= STAGES) ok = mbar_wait(bar_empty + 8 * s, ((i / STAGES) - 1) & 1, abort_flag);
         if (!ok) break;
-        const int t = solo ? i : i * n_cta + rank;
+        const int t = key_tile<WIN>(view, solo ? i : i * n_cta + rank);
         int blk, tok;
         if (p.block_table) {
           blk = p.block_table[(size_t)b * p.max_blocks + t / tiles_per_block];
+          if (WIN && (blk < 0 || blk >= p.n_blocks) && p.d_status) *p.d_status = SPECVLM_ERR_INVALID_ARG;   // the copy gives zeros
           tok = (t % tiles_per_block) * kTileTokens;
         } else {
           blk = b;
@@ -496,11 +518,11 @@ attn_rows16_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_consta
 
   if constexpr (SPLIT) {
     if (solo) {
-      if (rank == 0) rows16_consume<D, STAGES, NG, false>(p, smem, base, abort_flag, kv_len, n_my, 0, 1);
+      if (rank == 0) rows16_consume<D, STAGES, NG, false, WIN>(p, smem, base, abort_flag, view, n_my, 0, 1);
       return;
     }
   }
-  rows16_consume<D, STAGES, NG, SPLIT>(p, smem, base, abort_flag, kv_len, n_my, rank, n_cta);
+  rows16_consume<D, STAGES, NG, SPLIT, WIN>(p, smem, base, abort_flag, view, n_my, rank, n_cta);
 }
 
 // bar.sync 1 over n threads (whole warps) that also answers whether the predicate holds for all of them
@@ -540,7 +562,7 @@ struct SliceCfg {
   static_assert(SMEM <= 232448, "shared-memory plan does not fit");
 };
 
-template <int D>
+template <int D, bool WIN = false>
 __global__ void __launch_bounds__(32 * (4 * SliceCfg<D>::NG + 1), 1)
 attn_rows16_slices_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v,
                           const __grid_constant__ AttnTcParams p) {
@@ -571,7 +593,7 @@ attn_rows16_slices_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid
   }
   pdl_launch_next();
   pdl_wait();
-  if (warp == 0) plan_slice<kTileTokens>(p, prefix, slice, blockIdx.x, gridDim.x, lane);
+  if (warp == 0) plan_slice<kTileTokens, WIN>(p, prefix, slice, blockIdx.x, gridDim.x, lane);
   if (warp > 0 && warp < NW) unwritten_parts(p, blockIdx.x, D, tid - 32, 32 * (NW - 1));
   __syncthreads();
   const int hkv = p.n_kv_heads, cta = blockIdx.x;
@@ -587,14 +609,17 @@ attn_rows16_slices_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid
       const int tiles_per_block = p.block_table ? p.block_tokens / kTileTokens : 1;
       bool ok = true, told = false;
       int i = 0;
+      KeyView view = {};
       for (; !c.done() && ok; ++i) {
         const int s = i % STAGES;
         if (i >= STAGES) ok = warp_wait(bar_empty + 8 * s, ((i / STAGES) - 1) & 1, abort_flag);
         if (!ok) break;
-        const int t = c.sg.tile0 + c.j;
+        if (WIN && (i == 0 || c.j == 0)) view = key_view<WIN>(p, p.n_win, c.sg.b);
+        const int t = key_tile<WIN>(view, c.sg.tile0 + c.j);
         int blk = c.sg.b, tok = t * kTileTokens;
         if (p.block_table) {
           blk = p.block_table[(size_t)c.sg.b * p.max_blocks + t / tiles_per_block];
+          if (WIN && (blk < 0 || blk >= p.n_blocks) && p.d_status) *p.d_status = SPECVLM_ERR_INVALID_ARG;   // the copy gives zeros
           tok = (t % tiles_per_block) * kTileTokens;
         }
         const uint32_t full = bar_full + 8 * s, dst = base + s * STAGE_BYTES;
@@ -652,10 +677,10 @@ attn_rows16_slices_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid
   int i0 = 0;                                                          // slice index of the item's first tile
   while (!c.done()) {
     const Segment sg = c.sg;
-    const int kv_len = clamp_len(p.seq_lens[sg.b], p.max_seq_len);
+    const KeyView view = key_view<WIN>(p, p.n_win, sg.b);
     const size_t lb = (size_t)sg.layer * p.batch + sg.b;
     Rows16<D> st;
-    st.start(p, p.n_win, p.rows, lb, sg.g, kv_len, lane);
+    st.start(p, p.n_win, p.rows, lb, sg.g, view.len, lane);
     for (int j = (grp + NG - i0 % NG) % NG; alive && j < sg.n_tiles; j += NG) {
       const int i = i0 + j, s = i % STAGES;
       if (!mbar_wait(bar_full + 8 * s, (i / STAGES) & 1, abort_flag)) {
@@ -663,8 +688,8 @@ attn_rows16_slices_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid
         break;
       }
       const uint32_t k_base = base + s * STAGE_BYTES;
-      st.tile(k_base, k_base + TILE_BYTES, smem + s * STAGE_BYTES + TILE_BYTES, (sg.tile0 + j) * kTileTokens, kv_len,
-              p.scale_log2, cw, lane);
+      st.template tile<WIN>(p, k_base, k_base + TILE_BYTES, smem + s * STAGE_BYTES + TILE_BYTES, (sg.tile0 + j) * kTileTokens, view,
+                            cw, lane);
       __syncwarp();
       if (lane == 0) mbar_arrive(bar_empty + 8 * s);
     }
@@ -707,6 +732,7 @@ attn_rows16_slices_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid
 static std::atomic<int> g_forced_splits{0};
 
 constexpr int kRows16Max = 16;     // windows up to this many rows run on the 16-row kernels
+constexpr int kWindowMaxRows = 128;   // of specvlm_window_attn: what one CTA of the tcgen05 kernel takes
 
 // Time that one CTA takes for a tile, us.
 static double rows16_tile_us(const specvlm_kv_t* kv) {
@@ -805,13 +831,13 @@ static size_t rows16_ws_bytes(const specvlm_kv_t* kv, int32_t batch, int rows) {
 size_t attn_tc_ws_bytes(const specvlm_kv_t* kv, int32_t batch, int rows, int group);
 int32_t attn_tc_launch(const specvlm_kv_t* kv, const void* q, int32_t batch, int32_t n_q_heads, int32_t n_q,
                        float sm_scale, void* out, float* lse, void* ws, size_t ws_bytes, int32_t* d_status,
-                       cudaStream_t st, const int32_t* tree_parents);
+                       cudaStream_t st, const int32_t* tree_parents, const KeyWindow* win = nullptr);
 
-template <int D, int STAGES, int NG, bool SPLIT>
+template <int D, int STAGES, int NG, bool SPLIT, bool WIN>
 static int32_t launch_rows16_s(const CUtensorMap& tk, const CUtensorMap& tv, const AttnParams& p,
                                dim3 grid, cudaStream_t st) {
   constexpr int SMEM = STAGES * 2 * kTileTokens * D * 2 + 1024 + 16 * STAGES + 16 + (SPLIT ? 16 * 4 : 0);
-  auto kern = attn_rows16_kernel<D, STAGES, NG, SPLIT>;
+  auto kern = attn_rows16_kernel<D, STAGES, NG, SPLIT, WIN>;
   static std::atomic<uint64_t> attr_done{0};
   if (!smem_attr_once(attr_done, reinterpret_cast<const void*>(kern), SMEM)) return SPECVLM_ERR_CUDA;
   return launch_clusters_after(kern, grid, (int)grid.x, dim3(32 * (4 * NG + 1)), (size_t)SMEM, st, tk, tv, p);
@@ -820,20 +846,20 @@ static int32_t launch_rows16_s(const CUtensorMap& tk, const CUtensorMap& tv, con
 // Ring depth: 3 stages let two CTAs share an SM; a launch with no more CTAs than SMs would leave
 // every SM with one CTA and 96 KB of copies in flight, too little to cover the HBM latency, so it
 // takes 6 stages and two consumer groups instead.
-template <int D>
+template <int D, bool WIN>
 static int32_t launch_rows16(const CUtensorMap& tk, const CUtensorMap& tv, const AttnParams& p,
                              dim3 grid, cudaStream_t st) {
   const int64_t ctas = (int64_t)grid.x * grid.y * grid.z;
   constexpr int kDeep = D == 128 ? 6 : 12;
-  if (grid.x > 1) return launch_rows16_s<D, kDeep, 2, true>(tk, tv, p, grid, st);
-  return ctas <= sm_count() ? launch_rows16_s<D, kDeep, 2, false>(tk, tv, p, grid, st)
-                            : launch_rows16_s<D, 3, 1, false>(tk, tv, p, grid, st);
+  if (grid.x > 1) return launch_rows16_s<D, kDeep, 2, true, WIN>(tk, tv, p, grid, st);
+  return ctas <= sm_count() ? launch_rows16_s<D, kDeep, 2, false, WIN>(tk, tv, p, grid, st)
+                            : launch_rows16_s<D, 3, 1, false, WIN>(tk, tv, p, grid, st);
 }
 
-template <int D>
+template <int D, bool WIN>
 static int32_t launch_slices(const CUtensorMap& tk, const CUtensorMap& tv, const AttnTcParams& p, int ctas, cudaStream_t st) {
   using C = SliceCfg<D>;
-  auto kern = attn_rows16_slices_kernel<D>;
+  auto kern = attn_rows16_slices_kernel<D, WIN>;
   static std::atomic<uint64_t> attr_done{0};
   if (!smem_attr_once(attr_done, reinterpret_cast<const void*>(kern), C::SMEM)) return SPECVLM_ERR_CUDA;
   return launch_after(kern, dim3((unsigned)ctas), dim3(32 * (4 * C::NG + 1)), (size_t)C::SMEM, st, tk, tv, p);
@@ -847,7 +873,8 @@ __global__ void give_up_kernel(const __grid_constant__ AttnTcParams p, int gcta,
 
 static int32_t attn_common(const specvlm_kv_t* kv, const void* q, int32_t batch, int32_t n_q_heads,
                            int32_t n_q, float sm_scale, void* out, float* lse, void* ws,
-                           size_t ws_bytes, int32_t* d_status, void* stream, int lost_cta = -1, int32_t* n_ctas = nullptr) {
+                           size_t ws_bytes, int32_t* d_status, void* stream, int lost_cta = -1, int32_t* n_ctas = nullptr,
+                           const KeyWindow* win = nullptr) {
   int32_t rc = validate_kv(kv, batch, true);
   if (rc != SPECVLM_OK) return rc;
   if (!q || !out || n_q_heads < 1 || n_q < 1 || !(sm_scale > 0.f)) return SPECVLM_ERR_INVALID_ARG;
@@ -858,7 +885,7 @@ static int32_t attn_common(const specvlm_kv_t* kv, const void* q, int32_t batch,
   const int rows = group * n_q;
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   if (rows > kRows16Max)
-    return attn_tc_launch(kv, q, batch, n_q_heads, n_q, sm_scale, out, lse, ws, ws_bytes, d_status, st, nullptr);
+    return attn_tc_launch(kv, q, batch, n_q_heads, n_q, sm_scale, out, lse, ws, ws_bytes, d_status, st, nullptr, win);
 
   const int64_t lb64 = (int64_t)kv->n_layers * batch;
   if (lb64 > 65535 || kv->n_kv_heads > 65535) return SPECVLM_ERR_UNSUPPORTED_SHAPE;
@@ -868,8 +895,9 @@ static int32_t attn_common(const specvlm_kv_t* kv, const void* q, int32_t batch,
   rc = encode_kv_map(&tv, kv, kv->v, kTileTokens);
   if (rc != SPECVLM_OK) return rc;
 
+  const specvlm_kv_t sched = win ? win->view(kv, n_q) : *kv;
   int scratch_ctas;
-  const int ctas = rows16_slices(kv, batch, &scratch_ctas);
+  const int ctas = rows16_slices(&sched, batch, &scratch_ctas);
   if (scratch_ctas > 0) {
     if (!ws || (reinterpret_cast<uintptr_t>(ws) & 255u)) return SPECVLM_ERR_INVALID_ARG;
     if (ws_bytes < rows16_scratch_bytes(kv, scratch_ctas, rows)) return SPECVLM_ERR_WORKSPACE_TOO_SMALL;
@@ -879,7 +907,13 @@ static int32_t attn_common(const specvlm_kv_t* kv, const void* q, int32_t batch,
     AttnTcParams p = slice_params(kv, q, batch, n_q_heads, n_q, sm_scale, out, lse, d_status, 1, n_q, ws, sc);
     p.lost_cta = lost_cta;
     if (n_ctas) *n_ctas = ctas;
-    rc = kv->head_dim == 128 ? launch_slices<128>(tk, tv, p, ctas, st) : launch_slices<64>(tk, tv, p, ctas, st);
+    if (win) {
+      p.window = win->window;
+      p.n_sinks = win->n_sinks;
+      rc = kv->head_dim == 128 ? launch_slices<128, true>(tk, tv, p, ctas, st) : launch_slices<64, true>(tk, tv, p, ctas, st);
+    } else {
+      rc = kv->head_dim == 128 ? launch_slices<128, false>(tk, tv, p, ctas, st) : launch_slices<64, false>(tk, tv, p, ctas, st);
+    }
     return rc != SPECVLM_OK ? rc : attn_merge_launch(p, kv->head_dim, ctas, st);
   }
 
@@ -901,11 +935,15 @@ static int32_t attn_common(const specvlm_kv_t* kv, const void* q, int32_t batch,
   p.max_seq_len = kv->max_seq_len;
   p.scale_log2 = sm_scale * kLog2e;
   p.lost_cta = lost_cta;
+  p.window = win ? win->window : 0;
+  p.n_sinks = win ? win->n_sinks : 0;
+  p.n_blocks = kv->n_blocks;
 
-  const int n = rows16_cluster(kv, lb64 * kv->n_kv_heads, (kv->max_seq_len + kTileTokens - 1) / kTileTokens);
+  const int n = rows16_cluster(&sched, lb64 * kv->n_kv_heads, (sched.max_seq_len + kTileTokens - 1) / kTileTokens);
   dim3 grid((unsigned)n, (unsigned)kv->n_kv_heads, (unsigned)lb64);
   if (n_ctas) *n_ctas = (int32_t)(grid.x * grid.y * grid.z);
-  return kv->head_dim == 128 ? launch_rows16<128>(tk, tv, p, grid, st) : launch_rows16<64>(tk, tv, p, grid, st);
+  if (win) return kv->head_dim == 128 ? launch_rows16<128, true>(tk, tv, p, grid, st) : launch_rows16<64, true>(tk, tv, p, grid, st);
+  return kv->head_dim == 128 ? launch_rows16<128, false>(tk, tv, p, grid, st) : launch_rows16<64, false>(tk, tv, p, grid, st);
 }
 
 }  // namespace specvlm
@@ -976,6 +1014,24 @@ extern "C" int32_t specvlm_verify_attn(const specvlm_kv_t* kv, const void* q, in
   if (gamma < 0 || gamma > 8) return SPECVLM_ERR_UNSUPPORTED_SHAPE;
   return attn_common(kv, q, batch, n_q_heads, gamma + 1, sm_scale, out, lse_or_null, ws, ws_bytes,
                      d_status, stream);
+}
+
+extern "C" size_t specvlm_window_attn_workspace_bytes(const specvlm_kv_t* kv, int32_t batch, int32_t n_q_heads, int32_t n_q,
+                                                      int32_t window, int32_t n_sinks) {
+  if (!kv || n_q < 1 || window < 1 || n_sinks < 0 || kv->n_kv_heads < 1 || kv->max_seq_len < 1) return 0;
+  if ((int64_t)n_q_heads / kv->n_kv_heads * n_q > kWindowMaxRows) return 0;
+  const specvlm_kv_t view = KeyWindow(kv, window, n_sinks).view(kv, n_q);
+  return specvlm_attn_workspace_bytes(&view, batch, n_q_heads, n_q - 1);
+}
+
+extern "C" int32_t specvlm_window_attn(const specvlm_kv_t* kv, const void* q, int32_t batch, int32_t n_q_heads, int32_t n_q,
+                                       int32_t window, int32_t n_sinks, float sm_scale, void* out, float* lse_or_null,
+                                       void* ws, size_t ws_bytes, int32_t* d_status, void* stream) {
+  NvtxRange nvtx_range(__func__);
+  if (!kv || window < 1 || n_sinks < 0 || n_q < 1 || kv->n_kv_heads < 1) return SPECVLM_ERR_INVALID_ARG;
+  if (n_q > 9 || (int64_t)n_q_heads / kv->n_kv_heads * n_q > kWindowMaxRows) return SPECVLM_ERR_UNSUPPORTED_SHAPE;
+  const KeyWindow win(kv, window, n_sinks);
+  return attn_common(kv, q, batch, n_q_heads, n_q, sm_scale, out, lse_or_null, ws, ws_bytes, d_status, stream, -1, nullptr, &win);
 }
 
 extern "C" size_t specvlm_verify_tree_workspace_bytes(const specvlm_kv_t* kv, int32_t batch, int32_t n_q_heads,

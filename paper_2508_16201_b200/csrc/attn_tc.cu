@@ -66,7 +66,8 @@ struct TcCfg {
 // TREE: the window's visibility comes from per-token ancestor masks instead of the chain rule.
 // A template parameter, not a run-time branch: the chain kernel's code is untouched by the tree
 // variant (the softmax loop's speed proved sensitive to what is compiled around it).
-template <int D, int M, bool TREE>
+// WIN: a chain whose queries see a window and sinks (KeyView).
+template <int D, int M, bool TREE, bool WIN = false>
 __global__ void __launch_bounds__(kTcThreads, 1)
 attn_tc_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v,
                const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ AttnTcParams p) {
@@ -157,7 +158,7 @@ attn_tc_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__
   }
   pdl_wait();
   if (warp == 3) unwritten_parts(p, blockIdx.x, D, lane, 32);
-  if (warp == 0) plan_slice<kBigTokens>(p, prefix, slice, blockIdx.x, gridDim.x, lane);
+  if (warp == 0) plan_slice<kBigTokens, WIN>(p, prefix, slice, blockIdx.x, gridDim.x, lane);
   tc_fence_before_sync();
   __syncthreads();
   tc_fence_after_sync();
@@ -207,13 +208,14 @@ attn_tc_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__
                           sg.layer * p.batch + sg.b, policy_q);
           }
         }
-        const int n_sub_seq = (clamp_len(p.seq_lens[sg.b], p.max_seq_len) + kTileTokens - 1) / kTileTokens;
+        const KeyView view = key_view<WIN>(p, p.n_win, sg.b);
+        const int n_sub_seq = (view.len + kTileTokens - 1) / kTileTokens;
         const int32_t* table = p.block_table ? p.block_table + (size_t)sg.b * p.max_blocks : nullptr;
         int blk[2], blk_next[2] = {sg.b, sg.b};
         if (table) {
           const int s0 = 2 * sg.tile0;
-          blk_next[0] = __ldcg(table + s0 / subs_per_block);
-          blk_next[1] = s0 + 1 < n_sub_seq ? __ldcg(table + (s0 + 1) / subs_per_block) : 0;
+          blk_next[0] = __ldcg(table + key_tile<WIN>(view, s0) / subs_per_block);
+          blk_next[1] = s0 + 1 < n_sub_seq ? __ldcg(table + key_tile<WIN>(view, s0 + 1) / subs_per_block) : 0;
         }
         for (int j = 0; j < sg.n_tiles; ++j, ++i) {
           const int s0 = 2 * (sg.tile0 + j);                    // first sub-tile of this tile
@@ -221,8 +223,8 @@ attn_tc_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__
           blk[0] = blk_next[0];
           blk[1] = blk_next[1];
           if (table && j + 1 < sg.n_tiles) {                    // table entries of the next tile, one tile ahead
-            blk_next[0] = __ldcg(table + (s0 + 2) / subs_per_block);
-            blk_next[1] = s0 + 3 < n_sub_seq ? __ldcg(table + (s0 + 3) / subs_per_block) : 0;
+            blk_next[0] = __ldcg(table + key_tile<WIN>(view, s0 + 2) / subs_per_block);
+            blk_next[1] = s0 + 3 < n_sub_seq ? __ldcg(table + key_tile<WIN>(view, s0 + 3) / subs_per_block) : 0;
           }
           const int slot = i % n_ring;
           if (i >= n_ring) ok = warp_wait_soon(bar_empty + 8 * slot, ((i / n_ring) - 1) & 1, abort_flag);
@@ -230,7 +232,10 @@ attn_tc_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__
           if (leader) {
             mbar_arrive_expect_tx(bar_full + 8 * slot, n_sub * SUB_BYTES);
             for (int u = 0; u < n_sub; ++u) {
-              const int tok = table ? ((s0 + u) % subs_per_block) * kTileTokens : (s0 + u) * kTileTokens;
+              const int sub = key_tile<WIN>(view, s0 + u);
+              const int tok = table ? (sub % subs_per_block) * kTileTokens : sub * kTileTokens;
+              if (WIN && table && is_k && (blk[u] < 0 || blk[u] >= p.n_blocks) && p.d_status)
+                *p.d_status = SPECVLM_ERR_INVALID_ARG;          // the copy gives zeros
 #pragma unroll
               for (int h = 0; h < D / 64; ++h)
                 tma_load_5d(ring_sm + slot * 2 * SUB_BYTES + h * blk_stride + u * sub_stride, tm, bar_full + 8 * slot,
@@ -298,10 +303,12 @@ attn_tc_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__
       const uint64_t dv0 = umma_desc_sw128(v_sm, kTileTokens * 128, 1024);   // 64-channel blocks 8 KB apart
       bool ok = true;
       int n_sub_seq = 0, kv_len = 0;
+      KeyView view = {};
       for (int i = 0; i < n_my; ++i) {
         const int g = i & 1, vp = i % NVP;
         if (c.j == 0) {
-          kv_len = clamp_len(p.seq_lens[c.sg.b], p.max_seq_len);
+          view = key_view<WIN>(p, p.n_win, c.sg.b);
+          kv_len = view.len;
           n_sub_seq = (kv_len + kTileTokens - 1) / kTileTokens;
         }
         const int s0 = 2 * (c.sg.tile0 + c.j);
@@ -315,6 +322,21 @@ attn_tc_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__
             const int t = first + idx / (D / 8), c16 = idx % (D / 8);
             *reinterpret_cast<uint4*>(vt + (c16 >> 3) * (kTileTokens * 128) + t * 128 + (c16 & 7) * 16) =
                 make_uint4(0, 0, 0, 0);
+          }
+          fence_proxy_async();
+          __syncwarp();
+        }
+        if (WIN && s0 * kTileTokens < view.lo && (s0 + 2) * kTileTokens > p.n_sinks) {
+          // the same for the positions that no query sees, between the sinks and the window
+          for (int u = 0; u < n_sub; ++u) {
+            uint8_t* vt = big_ptr + C::OFF_V + vp * 2 * SUB_BYTES + u * SUB_BYTES;
+            const int at = (s0 + u) * kTileTokens;
+            const int first = p.n_sinks > at ? p.n_sinks - at : 0, last = view.lo - at < kTileTokens ? view.lo - at : kTileTokens;
+            for (int idx = lane; idx < (last - first) * (D / 8); idx += 32) {
+              const int t = first + idx / (D / 8), c16 = idx % (D / 8);
+              *reinterpret_cast<uint4*>(vt + (c16 >> 3) * (kTileTokens * 128) + t * 128 + (c16 & 7) * 16) =
+                  make_uint4(0, 0, 0, 0);
+            }
           }
           fence_proxy_async();
           __syncwarp();
@@ -387,13 +409,16 @@ attn_tc_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__
     while (!c.done()) {
       const Segment sg = c.sg;
       const int seg_idx = c.seg_idx;
-      const int kv_len = clamp_len(p.seq_lens[sg.b], p.max_seq_len);
+      const KeyView view = key_view<WIN>(p, p.n_win, sg.b);
+      const int kv_len = view.len;
       // Visibility of key `tok` for a row of query token t: every key before the window of the n_q
       // new tokens, and inside the window the positions whose bit is set in the row's mask -- bits
       // 0..t for a chain, the token's ancestors and itself for a tree.  Rows no item uses see nothing.
       // (A used row always has its own bit set, so a zero mask also marks an unused row.)
       // The chain keeps the equivalent limit form: key tok is visible to token t when tok < lim.
       const int win0 = kv_len - p.n_win;
+      // (WIN: tiles with positions that some query sees and another, or none, does not see)
+      auto window_edge = [&](int tok0) { return WIN && tok0 < view.lo + p.n_win - 1 && tok0 + kBigTokens > p.n_sinks; };
       float2* const seg_stats = stats;
       if constexpr (M == 128) {
         // ------------------------------------------------------------ 128-row windows: a thread owns a row
@@ -417,7 +442,7 @@ attn_tc_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__
         for (int j = (i0 + grp) & 1; j < sg.n_tiles; j += 2) {
           const int i = i0 + j;
           const int tile_tok0 = (sg.tile0 + j) * kBigTokens;
-          const bool need_mask = tile_tok0 + kBigTokens > win0 + (TREE ? 0 : 1);
+          const bool need_mask = tile_tok0 + kBigTokens > win0 + (TREE ? 0 : 1) || window_edge(tile_tok0);
           SM_WAIT(bar_s_full + 8 * grp, (i >> 1) & 1);
           tc_fence_after_sync();
           if (!warp_on) {
@@ -436,7 +461,10 @@ attn_tc_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__
             for (int h = 0; h < nh; ++h) {
               const uint64_t a0 = __shfl_sync(0xffffffffu, my_a, 16 * h + lr);
               const uint64_t a1 = __shfl_sync(0xffffffffu, my_a, 16 * h + lr + 8);
-              mask_s_half<TREE>(saddr + ((uint32_t)(16 * h) << 16), tile_tok0, win0, lc, a0, a1);
+              if constexpr (WIN)
+                mask_s_half_window(saddr + ((uint32_t)(16 * h) << 16), tile_tok0, lc, (int)a0, (int)a1, p.window, p.n_sinks);
+              else
+                mask_s_half<TREE>(saddr + ((uint32_t)(16 * h) << 16), tile_tok0, win0, lc, a0, a1);
             }
           }
           uint32_t va[16], vb[16];
@@ -566,7 +594,7 @@ attn_tc_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__
       for (int j = (i0 + grp) & 1; j < sg.n_tiles; j += 2) {
         const int i = i0 + j;
         const int tile_tok0 = (sg.tile0 + j) * kBigTokens;
-        const bool need_mask = tile_tok0 + kBigTokens > win0 + (TREE ? 0 : 1);
+        const bool need_mask = tile_tok0 + kBigTokens > win0 + (TREE ? 0 : 1) || window_edge(tile_tok0);
         SM_WAIT(bar_s_full + 8 * grp, (i >> 1) & 1);
         tc_fence_after_sync();
         if (nh == 0) {
@@ -582,6 +610,7 @@ attn_tc_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__
           const uint32_t saddr = tmem_base + ((uint32_t)(32 * quarter + 16 * h) << 16) + C::COL_S + grp * kBigTokens;
           if (__builtin_expect(need_mask, 0)) {
             if constexpr (TREE) mask_s_half<true>(saddr, tile_tok0, win0, lc, vis[0][0], vis[0][1]);
+            else if constexpr (WIN) mask_s_half_window(saddr, tile_tok0, lc, lim[0][0], lim[0][1], p.window, p.n_sinks);
             else mask_s_half<false>(saddr, tile_tok0, win0, lc, (uint64_t)lim[0][0], (uint64_t)lim[0][1]);
           }
           float mx0 = -INFINITY, mx1 = -INFINITY;
@@ -1027,6 +1056,7 @@ template <int D, int M>
 static int32_t launch_tc(const CUtensorMap& tk, const CUtensorMap& tv, const CUtensorMap& tq, const AttnTcParams& p,
                          int grid, cudaStream_t st) {
   constexpr int kSmem = TcCfg<D, M>::TOTAL;
+  if (p.window > 0) return launch_tc_kernel<attn_tc_kernel<D, M, false, true>>(kSmem, tk, tv, tq, p, grid, st);
   return p.parents ? launch_tc_kernel<attn_tc_kernel<D, M, true>>(kSmem, tk, tv, tq, p, grid, st)
                : launch_tc_kernel<attn_tc_kernel<D, M, false>>(kSmem, tk, tv, tq, p, grid, st);
 }
@@ -1037,7 +1067,7 @@ int32_t attn_pair_launch(const CUtensorMap& tk, const CUtensorMap& tv, const CUt
 
 int32_t attn_tc_launch(const specvlm_kv_t* kv, const void* q, int32_t batch, int32_t n_q_heads, int32_t n_q,
                        float sm_scale, void* out, float* lse, void* ws, size_t ws_bytes, int32_t* d_status,
-                       cudaStream_t st, const int32_t* tree_parents) {
+                       cudaStream_t st, const int32_t* tree_parents, const KeyWindow* win) {
   const int group = n_q_heads / kv->n_kv_heads;
   const int rows = group * n_q;
   if (group > 16 || batch > kSchedMaxBatch) return SPECVLM_ERR_UNSUPPORTED_SHAPE;
@@ -1045,9 +1075,10 @@ int32_t attn_tc_launch(const specvlm_kv_t* kv, const void* q, int32_t batch, int
   if (items > 0x3fffffff) return SPECVLM_ERR_UNSUPPORTED_SHAPE;
   if (!ws || (reinterpret_cast<uintptr_t>(ws) & 255u)) return SPECVLM_ERR_INVALID_ARG;
   // A window of more than 128 rows is cut into parts of equal numbers of query tokens that share one launch.
-  const SlicePlan pl = attn_tc_plan(kv, batch, group, n_q);
+  const specvlm_kv_t sched = win ? win->view(kv, n_q) : *kv;
+  const SlicePlan pl = attn_tc_plan(&sched, batch, group, n_q);
   const SliceScratch sc = tc_scratch(kv, pl, group);
-  if (ws_bytes < attn_tc_ws_bytes(kv, batch, rows, group)) return SPECVLM_ERR_WORKSPACE_TOO_SMALL;
+  if (ws_bytes < attn_tc_ws_bytes(&sched, batch, rows, group)) return SPECVLM_ERR_WORKSPACE_TOO_SMALL;
   if (tree_parents && n_q > kMaxTreeNodes) return SPECVLM_ERR_UNSUPPORTED_SHAPE;
   if (pl.q_per * group > 128) return SPECVLM_ERR_UNSUPPORTED_SHAPE;
   const int ctas = pl.ctas, n_parts = pl.n_parts;
@@ -1060,6 +1091,11 @@ int32_t attn_tc_launch(const specvlm_kv_t* kv, const void* q, int32_t batch, int
 
   AttnTcParams p = slice_params(kv, q, batch, n_q_heads, n_q, sm_scale, out, lse, d_status, n_parts, pl.q_per, ws, sc);
   p.parents = tree_parents;
+  if (win) {
+    p.window = win->window;
+    p.n_sinks = win->n_sinks;
+    if (n_parts > 1) return SPECVLM_ERR_UNSUPPORTED_SHAPE;
+  }
 
   CUtensorMap tq;
   rc = encode_q_map(&tq, q, kv->head_dim, group, n_q, pl.q_per, kv->n_kv_heads, (int64_t)kv->n_layers * batch);

@@ -28,6 +28,8 @@ struct AttnTcParams {
   int32_t lse_block;          // floats from one 64-channel block's LSEs to the next one's
   float scale_log2;           // sm_scale * log2(e)
   int32_t lost_cta;           // test hook (attn.cu): the CTA that gives up as if a wait had expired; -1 as a rule
+  int32_t window, n_sinks;    // specvlm_window_attn: the last keys and the first keys that a query sees
+  int32_t n_blocks;           // pages of the cache
 };
 
 constexpr float kRescaleThreshold = 8.f;   // log2 units
@@ -87,8 +89,6 @@ __device__ __forceinline__ float4 ldg_cg_f32x4(const float* p) {
   return v;
 }
 
-__device__ __forceinline__ int clamp_len(int n, int max_len) { return n < 0 ? 0 : (n > max_len ? max_len : n); }
-
 // Cold paths of the softmax loop, kept out of line: the loop's code has to stay small enough for
 // the instruction cache (with the mask logic inline the 128-row variant ran 25 % slower, although
 // only one or two tiles of an item ever need a mask).
@@ -124,6 +124,29 @@ __device__ __noinline__ void mask_s_half(uint32_t saddr, int tile_tok0, int win0
         const int n_vis = (int)a[e] - tile_tok0 - 64 * c;       // visible columns of the block
         mk[e] = (n_vis <= 0 ? 0ull : (n_vis >= 64 ? ~0ull : ((1ull << n_vis) - 1ull))) >> lc;
       }
+    }
+    uint32_t v[32];
+    tmem_ld_16x256b_x8(saddr + 64 * c, v);
+    tmem_ld_wait();
+#pragma unroll
+    for (int k = 0; k < 32; ++k)
+      if (!((mk[(k >> 1) & 1] >> ((k >> 2) * 8 + (k & 1))) & 1ull)) v[k] = 0xff800000u;   // -inf
+    tmem_st_16x256b_x8(saddr + 64 * c, v);
+  }
+  tmem_st_wait();
+}
+
+// The same for a chain whose queries see a window and sinks (KeyView): lim0, lim1 = the rows' key limits, 0 for an unused row.
+static __device__ __noinline__ void mask_s_half_window(uint32_t saddr, int tile_tok0, int lc, int lim0, int lim1, int window,
+                                                       int n_sinks) {
+  auto below = [](int n) { return n <= 0 ? 0ull : (n >= 64 ? ~0ull : ((1ull << n) - 1ull)); };
+#pragma unroll 1
+  for (int c = 0; c < 2; ++c) {
+    uint64_t mk[2];
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+      const int lim = e ? lim1 : lim0, base = tile_tok0 + 64 * c;
+      mk[e] = (below(lim - base) & (~below(lim - window - base) | below(n_sinks - base))) >> lc;
     }
     uint32_t v[32];
     tmem_ld_16x256b_x8(saddr + 64 * c, v);
@@ -187,7 +210,7 @@ __device__ __noinline__ void rescale_o_half(uint32_t oaddr, float f0, float f1) 
 
 // Running sum of the tiles (of TILE tokens) per sequence, by one warp: prefix[b] = tiles of the sequences before b.
 // Returns whether some sequence has no token.
-template <int TILE>
+template <int TILE, bool WIN>
 __device__ __forceinline__ bool tile_prefix(const AttnTcParams& p, int* prefix, int lane) {
   int carry = 0;
   bool empty = false;
@@ -195,7 +218,7 @@ __device__ __forceinline__ bool tile_prefix(const AttnTcParams& p, int* prefix, 
     const int b = b0 + lane;
     int v = 0;
     if (b < p.batch) {
-      v = (clamp_len(p.seq_lens[b], p.max_seq_len) + TILE - 1) / TILE;
+      v = (key_view<WIN>(p, p.n_win, b).len + TILE - 1) / TILE;
       empty |= v == 0;
     }
 #pragma unroll
@@ -221,9 +244,9 @@ struct CtaSlice {
 constexpr int kPlanBytes = (int)sizeof(CtaSlice) + (kSchedAlignedBatch + 1) * 4;   // with the CTAs per sequence behind it
 
 // The plan of CTA `cta` of `ctas`, by one warp: the running sums of the tiles and the CTA's slice, to shared memory.
-template <int TILE>
+template <int TILE, bool WIN = false>
 __device__ __forceinline__ void plan_slice(const AttnTcParams& p, int* prefix, CtaSlice* out, int cta, int ctas, int lane) {
-  const bool empty = tile_prefix<TILE>(p, prefix, lane);
+  const bool empty = tile_prefix<TILE, WIN>(p, prefix, lane);
   __syncwarp();
   const int per_head = prefix[p.batch], lh = p.n_layers * p.n_kv_heads;
   const int64_t total = (int64_t)lh * per_head;
@@ -359,8 +382,24 @@ inline AttnTcParams slice_params(const specvlm_kv_t* kv, const void* q, int32_t 
   p.lse_block = 2 * sc.grid * p.rows;
   p.scale_log2 = sm_scale * kLog2e;
   p.lost_cta = -1;
+  p.window = p.n_sinks = 0;
+  p.n_blocks = kv->n_blocks;
   return p;
 }
+
+// The window of specvlm_window_attn on the host's side: what the queries see, and the longest sequence's positions (KeyView),
+// which size the launch.
+struct KeyWindow {
+  int32_t window, n_sinks;
+  KeyWindow(const specvlm_kv_t* kv, int32_t window, int32_t n_sinks)
+      : window(window < kv->max_seq_len ? window : kv->max_seq_len), n_sinks(n_sinks < kv->max_seq_len ? n_sinks : kv->max_seq_len) {}
+  specvlm_kv_t view(const specvlm_kv_t* kv, int32_t n_q) const {
+    specvlm_kv_t v = *kv;
+    const int64_t most = (int64_t)round_up((size_t)n_sinks, kTileTokens) + kTileTokens - 1 + window + n_q - 1;
+    if (most < v.max_seq_len) v.max_seq_len = (int32_t)most;
+    return v;
+  }
+};
 
 // How a launch on slices of a given window is laid out: `ctas` CTAs in each of n_parts sets (0: a CTA per item).
 struct SlicePlan {

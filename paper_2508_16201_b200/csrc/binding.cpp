@@ -233,6 +233,7 @@ PyMethodDef g_methods[] = {
     SPECVLM_ENTRY(append_kv, Kv, Ptr, Ptr, I32, I32, Ptr, Ptr),
     SPECVLM_ENTRY(rollback_kv, Ptr, Ptr, I32, I32, Ptr),
     SPECVLM_ENTRY(compact_tree_kv, Kv, Ptr, Ptr, I32, I32, Ptr, Ptr),
+    SPECVLM_ENTRY(window_attn, Kv, Ptr, I32, I32, I32, I32, I32, Float, Ptr, Ptr, Ptr, Size, Ptr),
     SPECVLM_ENTRY(rope_append_kv, Kv, Rope, Rows, Rows, Rows, Rows, I32, I32, I32, Ptr, Ptr, Ptr, I32, Ptr),
     SPECVLM_ENTRY(reserve_pages, Kv, Ptr, Ptr, I32, I32, Ptr, Ptr, Size, Ptr),
     SPECVLM_ENTRY(release_pages, Kv, Ptr, Ptr, I32, I32, I32, Ptr),

@@ -69,6 +69,7 @@ EXPORTS = [
     "specvlm_append_kv", "specvlm_rollback_kv",
     "specvlm_verify_tree_workspace_bytes", "specvlm_verify_tree_attn", "specvlm_accept_tree",
     "specvlm_compact_tree_kv",
+    "specvlm_window_attn_workspace_bytes", "specvlm_window_attn",
     "specvlm_rope_turns", "specvlm_rope_frequencies", "specvlm_rope_append_kv",
     "specvlm_pages_workspace_bytes", "specvlm_reserve_pages", "specvlm_release_pages", "specvlm_fork_pages",
     "specvlm_compact_pages", "specvlm_debug_poison_shared_memory", "specvlm_debug_wait_timeout",
@@ -142,6 +143,11 @@ def lib():
         L.specvlm_append_kv.argtypes = [kvp, c_void_p, c_void_p, c_int32, c_int32, c_void_p, c_void_p, c_void_p]
         L.specvlm_rollback_kv.restype = c_int32
         L.specvlm_rollback_kv.argtypes = [c_void_p, c_void_p, c_int32, c_int32, c_void_p, c_void_p]
+        L.specvlm_window_attn_workspace_bytes.restype = c_size_t
+        L.specvlm_window_attn_workspace_bytes.argtypes = [kvp, c_int32, c_int32, c_int32, c_int32, c_int32]
+        L.specvlm_window_attn.restype = c_int32
+        L.specvlm_window_attn.argtypes = [kvp, c_void_p, c_int32, c_int32, c_int32, c_int32, c_int32, c_float, c_void_p, c_void_p,
+                                          c_void_p, c_size_t, c_void_p, c_void_p]
         rowsp = POINTER(RowsStruct)
         L.specvlm_rope_turns.restype = c_int32
         L.specvlm_rope_turns.argtypes = [POINTER(ctypes.c_double), c_int32, POINTER(ctypes.c_uint64)]
@@ -326,6 +332,28 @@ def verify_attn(kv: KvCache, q: torch.Tensor, gamma: int, sm_scale: float,
                               d_status)
     if rc:
         _check(rc, "specvlm_verify_attn")
+    return out
+
+
+def window_attn_workspace_bytes(kv: KvCache, batch: int, n_q_heads: int, n_q: int, window: int, n_sinks: int) -> int:
+    return int(lib().specvlm_window_attn_workspace_bytes(byref(kv.struct), batch, n_q_heads, n_q, window, n_sinks))
+
+
+def window_attn(kv: KvCache, q: torch.Tensor, window: int, n_sinks: int, sm_scale: float, out: torch.Tensor | None = None,
+                lse: torch.Tensor | None = None, ws: torch.Tensor | None = None,
+                d_status: torch.Tensor | None = None) -> torch.Tensor:
+    """q, out: bf16 [n_layers][batch][n_q][n_q_heads][head_dim]; a query sees the last ``window`` keys up to its own and the
+    first ``n_sinks``."""
+    L, B, NQ, Hq, D = q.shape
+    assert q.is_contiguous() and q.dtype == torch.bfloat16 and L == kv.n_layers and D == kv.head_dim
+    if out is None:
+        out = torch.empty_like(q)
+    if ws is None:
+        ws = _ws(window_attn_workspace_bytes(kv, B, Hq, NQ, window, n_sinks), q.device)
+    rc = native().window_attn(addressof(kv.struct), q, B, Hq, NQ, window, n_sinks, float(sm_scale), out, lse, ws, ws.numel(),
+                              d_status)
+    if rc:
+        _check(rc, "specvlm_window_attn")
     return out
 
 

@@ -167,3 +167,31 @@ def test_oracle_window_is_the_definition():
     out, lse = rolling.attention_window(q, k, v, 9, 1, 0, 0.3)                       # each token sees itself alone
     np.testing.assert_allclose(out[1, 3], v[1, 8])
     np.testing.assert_allclose(lse[0, 0], 0.3 * (q[0, 0] @ k[0, 7]))
+
+
+def test_window_refusals():
+    def call(kv=None, q=0x3000, batch=2, heads=8, n_q=1, window=5, sinks=0, scale=0.1, out=0x4000, ws=0x10000, size=1 << 26):
+        return specvlm.lib().specvlm_window_attn(ctypes.byref(kv or _kv()), q, batch, heads, n_q, window, sinks, scale, out, None,
+                                                 ws, size, None, None)
+    assert call(window=0) == BAD and call(window=-1) == BAD and call(sinks=-1) == BAD and call(n_q=0) == BAD
+    assert call(q=None) == BAD and call(out=None) == BAD and call(q=0x3008) == BAD and call(scale=0.0) == BAD and call(scale=math.nan) == BAD
+    assert call(heads=0) == BAD and call(heads=9) == BAD and call(batch=0) == BAD
+    assert call(n_q=10) == SHAPE and call(heads=4 * 17) == SHAPE
+    assert call(heads=4 * 16, n_q=9) == SHAPE                                    # 144 rows
+    assert call(heads=4 * 8, n_q=6, batch=128) == SHAPE
+    assert call(heads=4 * 8, n_q=6, ws=None) == BAD and call(heads=4 * 8, n_q=6, ws=0x10010) == BAD
+    assert call(heads=4 * 8, n_q=6, size=16) == SMALL
+    assert call(kv=_with(_kv, head_dim=96)) == SHAPE and call(kv=_with(_kv, n_kv_heads=0)) == BAD
+    size = lambda *a: specvlm.lib().specvlm_window_attn_workspace_bytes(ctypes.byref(_kv()), *a)  # noqa: E731
+    assert size(2, 32, 6, 5, 0) > 0 and size(2, 8, 1, 5, 0) > 0
+    for bad in ((0, 8, 1, 5, 0), (2, 8, 0, 5, 0), (2, 8, 1, 0, 0), (2, 8, 1, 5, -1), (2, 64, 9, 5, 0), (2, 9, 1, 5, 0), (2, 8, 10, 5, 0)):
+        assert size(*bad) == 0, bad
+
+
+def test_a_window_workspace_is_no_larger_than_the_whole_caches():
+    for tokens in (64, 1000, 6400, 50000):
+        kv = _with(_kv, max_seq_len=tokens)
+        for heads, n_q in ((28, 1), (32, 6), (64, 8)):
+            whole = specvlm.lib().specvlm_attn_workspace_bytes(ctypes.byref(kv), 4, heads, n_q - 1)
+            for window, sinks in ((1, 0), (512, 64), (4096, 4), (2 ** 31 - 1, 2 ** 31 - 1)):
+                assert specvlm.lib().specvlm_window_attn_workspace_bytes(ctypes.byref(kv), 4, heads, n_q, window, sinks) <= whole
