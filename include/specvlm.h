@@ -397,7 +397,7 @@ int32_t specvlm_window_attn(const specvlm_kv_t* kv, const void* q, int32_t batch
  * sections[0] pairs take axis 0, the next sections[1] axis 1, the rest axis 2; the sections add up to rot_dim / 2.
  */
 typedef struct specvlm_rope {
-  const uint64_t* turns;        /* device [rot_dim / 2]                                      */
+  const uint64_t* turns;        /* device [rot_dim / 2], 16-byte aligned                     */
   int32_t rot_dim;              /* rotated channels: a multiple of 16, 16 .. head_dim        */
   int32_t interleaved;
   int32_t n_axes;               /* 1 .. 3                                                    */

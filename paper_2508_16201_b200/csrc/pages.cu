@@ -80,6 +80,7 @@ struct ReservePlan {
   int first[kPagesMaxBatch];          // its slot
   int before[kPagesMaxBatch + 1];     // slots of the sequences before
   uint8_t copied[kPagesMaxBatch];     // the begun page is replaced by a copy
+  int list[kPlanThreads];             // the free pages to hand out, where a round of slots is all there is
 };
 
 __global__ void __launch_bounds__(kPlanThreads) reserve_plan_kernel(const __grid_constant__ PagesParams p) {
@@ -133,7 +134,8 @@ __global__ void __launch_bounds__(kPlanThreads) reserve_plan_kernel(const __grid
     if (old < 0 || old >= p.n_blocks) old = -1;
   };
   const bool one_round = total_slots <= kPlanThreads;
-  int total = 0, b = 0, j = 0, old = -1, nth = -1;
+  int32_t* const list = one_round ? sm.list : p.list;
+  int total = 0, b = 0, j = 0, old = -1, nth = -1, copy_at = 0, n_copies = 0;
   for (int i0 = 0; i0 < total_slots; i0 += kPlanThreads) {
     const int i = i0 + tid;
     bool fresh = false;
@@ -141,15 +143,17 @@ __global__ void __launch_bounds__(kPlanThreads) reserve_plan_kernel(const __grid
       look(i, b, j, old);
       fresh = old < 0 || (j == sm.first[b] && sm.begun[b] >= 0 ? sm.copied[b] != 0 : p.ref[old] > 1);
     }
+    // slots in the lower half; in the upper one the copies, whose list is in the order of the sequences
     int here;
-    const int at = total + block_scan(fresh ? 1 : 0, sm.warp_sums, here);
-    nth = fresh ? at : -1;
+    const int at = block_scan((fresh ? 1 : 0) + (i0 == 0 && copied ? 0x10000 : 0), sm.warp_sums, here);
+    nth = fresh ? total + (at & 0xffff) : -1;
     if (!one_round && i < total_slots) p.order[i] = nth;
-    total += here;
+    total += here & 0xffff;
+    if (i0 == 0) {
+      copy_at = at >> 16;
+      n_copies = here >> 16;
+    }
   }
-  // the copies' place in their list, in the order of the sequences
-  int n_copies;
-  const int copy_at = block_scan(copied ? 1 : 0, sm.warp_sums, n_copies);
   // the lowest free pages, as many as are needed
   int found = 0;
   for (int base0 = 0; base0 < p.n_blocks && found < total; base0 += kPlanThreads * kPagesPerThread) {
@@ -163,7 +167,7 @@ __global__ void __launch_bounds__(kPlanThreads) reserve_plan_kernel(const __grid
 #pragma unroll
     for (int i = 0; i < kPagesPerThread; ++i)
       if (c[i] == 0) {
-        if (at < total) p.list[at] = base + i;
+        if (at < total) list[at] = base + i;
         ++at;
       }
     found += here;
@@ -184,7 +188,7 @@ __global__ void __launch_bounds__(kPlanThreads) reserve_plan_kernel(const __grid
       nth = p.order[i];
     }
     if (i < total_slots && nth >= 0) {
-      const int fresh = p.list[nth];
+      const int fresh = list[nth];
       p.table[(size_t)b * p.max_blocks + j] = fresh;
       p.ref[fresh] = 1;
       if (old >= 0) atomicSub(p.ref + old, 1);

@@ -6,7 +6,7 @@
 //
 // Angles: a position times a frequency in radians loses the angle's digits to the whole turns (position 50 000 in fp32: 2e-3
 // radians).  Here frequencies are fractions of a turn in 64-bit fixed point, and position * fraction modulo 2^64 is the exact
-// fraction of the angle; its upper 32 bits go to fp32 (2^-25 of a turn at most).
+// fraction of the angle, of which the upper 32 bits are used.
 //
 // Lengths and block tables are device data: checked before they become part of an address (see cache.cu).
 #include <math.h>
@@ -42,116 +42,222 @@ struct RopeParams {
   float factor;
 };
 
-// First cache position and number of a sequence's new tokens; false if it is to be left alone.
-__device__ __forceinline__ bool rope_range(const RopeParams& p, int b, int& start, int& n) {
-  n = p.new_lens ? p.new_lens[b] : p.n_new;
-  const int len = p.seq_lens[b];
+// First cache position of the n new tokens of a sequence of length `len`; false if it is to be left alone.
+__device__ __forceinline__ bool rope_range(const RopeParams& p, int n, int len, int& start) {
   if (n < 0 || n > p.n_new || len < 0 || len > p.max_seq_len) return false;
   start = p.counted ? len - n : len;
   return start >= 0 && n <= p.max_seq_len - start;
 }
-
-__device__ __forceinline__ float2 bf16x2_to_f2(uint32_t x) {
-  return make_float2(__uint_as_float(x << 16), __uint_as_float(x & 0xffff0000u));
+__device__ __forceinline__ void rope_count(const RopeParams& p, int b) {       // (the append has reported the others)
+  const int n = p.new_lens ? p.new_lens[b] : p.n_new, len = p.seq_lens[b];
+  int start;
+  if (rope_range(p, n, len, start)) p.seq_lens[b] = start + n;
 }
 
-// The 8 pairs of two 16-byte vectors: the e-th channels of both (half layout), or neighbours (interleaved).
+__device__ __forceinline__ uint64_t bf16x2_to_f2(uint32_t x) {
+  return f2_pack(__uint_as_float(x << 16), __uint_as_float(x & 0xffff0000u));
+}
+__device__ __forceinline__ uint32_t f2_to_bf16x2(uint64_t v) {
+  float lo, hi;
+  f2_unpack(v, lo, hi);
+  return pack_bf16x2(lo, hi);
+}
+__device__ __forceinline__ uint64_t f2_mul(uint64_t a, uint64_t b) {
+  uint64_t d;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+  return d;
+}
+__device__ __forceinline__ uint64_t f2_swap(uint64_t v) {
+  float lo, hi;
+  f2_unpack(v, lo, hi);
+  return f2_pack(hi, lo);
+}
+
+// The 8 pairs of two 16-byte vectors, two at a time.  Half layout: the e-th channels of both; c and s hold the cosines and sines of
+// pairs 2 w and 2 w + 1.  Interleaved: neighbours; c and s hold those of pair w twice, the first sine negated.
 template <bool INTER>
-__device__ __forceinline__ void turn_pairs(uint4& x, uint4& y, const float (&c)[8], const float (&s)[8]) {
+__device__ __forceinline__ void turn_pairs(uint4& x, uint4& y, const uint64_t (&c)[INTER ? 8 : 4], const uint64_t (&s)[INTER ? 8 : 4]) {
   uint32_t* const xw = reinterpret_cast<uint32_t*>(&x);
   uint32_t* const yw = reinterpret_cast<uint32_t*>(&y);
 #pragma unroll
   for (int w = 0; w < 4; ++w) {
-    const float2 a = bf16x2_to_f2(xw[w]), b = bf16x2_to_f2(yw[w]);
+    const uint64_t a = bf16x2_to_f2(xw[w]), b = bf16x2_to_f2(yw[w]);
     if constexpr (INTER) {
-      xw[w] = pack_bf16x2(a.x * c[w] - a.y * s[w], a.y * c[w] + a.x * s[w]);
-      yw[w] = pack_bf16x2(b.x * c[w + 4] - b.y * s[w + 4], b.y * c[w + 4] + b.x * s[w + 4]);
+      xw[w] = f2_to_bf16x2(f2_fma(a, c[w], f2_mul(f2_swap(a), s[w])));
+      yw[w] = f2_to_bf16x2(f2_fma(b, c[w + 4], f2_mul(f2_swap(b), s[w + 4])));
     } else {
-      xw[w] = pack_bf16x2(a.x * c[2 * w] - b.x * s[2 * w], a.y * c[2 * w + 1] - b.y * s[2 * w + 1]);
-      yw[w] = pack_bf16x2(b.x * c[2 * w] + a.x * s[2 * w], b.y * c[2 * w + 1] + a.y * s[2 * w + 1]);
+      const uint64_t minus_b = b ^ 0x8000000080000000ull;
+      xw[w] = f2_to_bf16x2(f2_fma(a, c[w], f2_mul(minus_b, s[w])));
+      yw[w] = f2_to_bf16x2(f2_fma(b, c[w], f2_mul(a, s[w])));
     }
   }
 }
 
-constexpr int kRopeThreads = 256, kRopeOneThreads = 1024, kRopeOneTokens = 8;
+// Sine and cosine of a fraction of a turn (2^32 = a whole one): reduced exactly to an eighth of a turn either way, there
+// polynomials of degree 7 and 8 (least maximum error, fitted for this file: 3.1e-9 and 5e-11), together with their rounding off
+// by at most 1.5 x 2^-24.
+__device__ __forceinline__ void turn_sincos(uint32_t turn, float& s, float& c) {
+  const uint32_t quarter = (turn + 0x20000000u) >> 30;
+  const float x = (float)(int32_t)(turn - (quarter << 30)) * 2.3283064365386963e-10f;      // 2^-32
+  const float u = x * x;
+  float sn = fmaf(u, -75.40206909179688f, 81.5925521850586f);
+  sn = fmaf(u, sn, -41.3416633605957f);
+  sn = x * fmaf(u, sn, 6.2831854820251465f);
+  float cs = fmaf(u, 59.22040557861328f, -85.44285583496094f);
+  cs = fmaf(u, cs, 64.93931579589844f);
+  cs = fmaf(u, cs, -19.739208221435547f);
+  cs = fmaf(u, cs, 1.0f);
+  const bool odd = quarter & 1u;
+  s = odd ? cs : sn;
+  c = odd ? sn : cs;
+  s = quarter & 2u ? -s : s;
+  c = (quarter + 1u) & 2u ? -c : c;
+}
 
+constexpr int kRopeThreads = 128, kRopeOneThreads = 512, kRopeOneTokens = 8;
+constexpr int kRopeCtas = 8;                       // on an SM: 64 registers a thread
+constexpr int kRopeWarps = 16;                     // on an SM: with fewer tokens several warps share one
+constexpr int kRopeBatch = 2;         // rounds whose loads are in flight together
+
+// A warp's rounds are the query rows first and then the key and value rows; those of a token are dealt out to `share` warps.
 template <int D, bool INTER>
 __device__ __forceinline__ void rope_rows(const RopeParams& p, uint32_t warp, int lane) {
-  constexpr int UNITS = D / 16, ROWS = 32 / UNITS;  // threads of a row, rows of a warp's round
+  constexpr int UNITS = D / 16, ROWS = 32 / UNITS;  // threads of a row, rows of a round
   const uint32_t token = warp / (uint32_t)p.share, lb = token / (uint32_t)p.n_new;
   const int part = (int)(warp - token * p.share), t = (int)(token - lb * p.n_new);
   const int layer = (int)(lb / (uint32_t)p.batch), b = (int)(lb - (uint32_t)layer * p.batch);
-  const int u = lane % UNITS;
+  const int u = lane % UNITS, sub = lane / UNITS, step = ROWS * p.share;
   const bool rotates = u < p.n_rot;
-  const int v0 = !INTER && rotates ? u : 2 * u, v1 = !INTER && rotates ? u + p.n_rot : 2 * u + 1;   // this thread's vectors
-  const int n_rows = p.n_q_heads + 2 * p.n_kv_heads, step = ROWS * p.share;
+  const int v0 = !INTER && rotates ? u : 2 * u, dv = !INTER && rotates ? p.n_rot : 1;      // this thread's vectors: v0, v0 + dv
+  const uint4* q = p.q + layer * p.q_layer + b * p.q_batch + t * p.q_token + v0;
 
-  int start, n;
-  const bool ok = rope_range(p, b, start, n);
-  if (!ok) {
+  // All loads that depend on nothing are asked for together: the launch is one or two waves of short warps, whose time
+  // is the number of round trips to memory one after the other.
+  const int n_asked = p.new_lens ? p.new_lens[b] : p.n_new, len = p.seq_lens[b];
+  int pos[3] = {0, 0, 0};
+  ulonglong2 turns[4];
+  if (rotates) {
+    if (p.positions) {
+      const int32_t* const at = p.positions + (size_t)b * p.n_new + t;
+      const size_t axis = (size_t)p.batch * p.n_new;
+#pragma unroll
+      for (int a = 0; a < 3; ++a)
+        if (a < p.n_axes) pos[a] = at[a * axis];
+    }
+#pragma unroll
+    for (int e = 0; e < 4; ++e) turns[e] = reinterpret_cast<const ulonglong2*>(p.turns)[4 * u + e];
+  }
+  uint4 x[kRopeBatch], y[kRopeBatch];
+  int row = part * ROWS + sub;
+  const int64_t q_step = step * p.q_head;
+  const uint4* src = q + row * p.q_head;
+#pragma unroll
+  for (int i = 0; i < kRopeBatch; ++i) {            // (the rows of padding are dropped)
+    if (row + i * step < p.n_q_heads) {
+      x[i] = src[0];
+      y[i] = src[dv];
+    }
+    src += q_step;
+  }
+
+  int start;
+  if (!rope_range(p, n_asked, len, start)) {
     if (lane == 0 && p.d_status) *p.d_status = SPECVLM_ERR_INVALID_ARG;
     return;
   }
-  if (t >= n) return;
-  float c[8], s[8];
-  if (rotates) {
-    int pos[3] = {start + t, start + t, start + t};
-    if (p.positions) {
-#pragma unroll
-      for (int a = 0; a < 3; ++a)
-        if (a < p.n_axes) pos[a] = p.positions[((size_t)a * p.batch + b) * p.n_new + t];
-    }
-#pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      const int i = 8 * u + e;
-      const int at = p.n_axes == 1 || i < p.axis1 ? pos[0] : i < p.axis2 ? pos[1] : pos[2];
-      const uint64_t turn = (uint64_t)(int64_t)at * p.turns[i];
-      sincospif((float)(int32_t)(turn >> 32) * 4.656612873077393e-10f, &s[e], &c[e]);    // 2^-31: half turns
-      s[e] *= p.factor;
-      c[e] *= p.factor;
-    }
-  }
+  if (t >= n_asked) return;
   const int at = start + t;
   int blk = b, off = at;
   bool stored = true;
   if (p.table) {
-    blk = p.table[(size_t)b * p.max_blocks + at / p.block_tokens];
-    off = at % p.block_tokens;
+    const int nth = (int)((uint32_t)at / (uint32_t)p.block_tokens);
+    blk = p.table[(size_t)b * p.max_blocks + nth];
+    off = at - nth * p.block_tokens;
     stored = blk >= 0 && blk < p.n_blocks;
     if (!stored && lane == 0 && p.d_status) *p.d_status = SPECVLM_ERR_INVALID_ARG;
   }
-  const int64_t dst = layer * p.s_layer + blk * p.s_block + off * p.s_token;
-  const uint4* const q = p.q + layer * p.q_layer + b * p.q_batch + t * p.q_token;
-  uint4* const o = p.q_out + layer * p.o_layer + b * p.o_batch + t * p.o_token;
-  const uint4* const nk = p.new_k + layer * p.k_layer + b * p.k_batch + t * p.k_token;
-  const uint4* const nv = p.new_v + layer * p.v_layer + b * p.v_batch + t * p.v_token;
-#pragma unroll 4
-  for (int row = part * ROWS + lane / UNITS; row < n_rows; row += step) {
-    const int h = row - p.n_q_heads, g = h - p.n_kv_heads;
-    const uint4* src = h < 0 ? q + row * p.q_head : g < 0 ? nk + h * p.k_head : nv + g * p.v_head;
-    uint4* to = h < 0 ? o + row * p.o_head : g < 0 ? p.k + dst + h * p.s_head : p.v + dst + g * p.s_head;
-    uint4 x = src[v0], y = src[v1];
-    if (rotates && g < 0) turn_pairs<INTER>(x, y, c, s);
-    if (h < 0 || stored) {
-      to[v0] = x;
-      to[v1] = y;
+  uint64_t c[INTER ? 8 : 4], s[INTER ? 8 : 4];
+  if (rotates) {
+    if (!p.positions) pos[0] = pos[1] = pos[2] = at;
+    float cs[8], sn[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const int i = 8 * u + e;
+      const int where = i < p.axis1 ? pos[0] : i < p.axis2 ? pos[1] : pos[2];
+      turn_sincos((uint32_t)(((uint64_t)(int64_t)where * (e & 1 ? turns[e >> 1].y : turns[e >> 1].x)) >> 32), sn[e], cs[e]);
+      sn[e] *= p.factor;
+      cs[e] *= p.factor;
+    }
+#pragma unroll
+    for (int e = 0; e < (INTER ? 8 : 4); ++e) {
+      c[e] = INTER ? f2_pack(cs[e], cs[e]) : f2_pack(cs[2 * e], cs[2 * e + 1]);
+      s[e] = INTER ? f2_pack(-sn[e], sn[e]) : f2_pack(sn[2 * e], sn[2 * e + 1]);
+    }
+  }
+  // queries
+  const int64_t o_step = step * p.o_head;
+  uint4* to = p.q_out + layer * p.o_layer + b * p.o_batch + t * p.o_token + row * p.o_head + v0;
+  while (row < p.n_q_heads) {
+#pragma unroll
+    for (int i = 0; i < kRopeBatch; ++i) {
+      if (row + i * step < p.n_q_heads) {
+        if (rotates) turn_pairs<INTER>(x[i], y[i], c, s);
+        to[0] = x[i];
+        to[dv] = y[i];
+      }
+      to += o_step;
+    }
+    row += kRopeBatch * step;
+#pragma unroll
+    for (int i = 0; i < kRopeBatch; ++i) {
+      if (row + i * step < p.n_q_heads) {
+        x[i] = src[0];
+        y[i] = src[dv];
+      }
+      src += q_step;
+    }
+  }
+  // keys and values, to the cache: their rounds go on where those of the queries end
+  if (!stored) return;
+  const int q_rounds = (p.n_q_heads + ROWS - 1) / ROWS;
+  int first = part - q_rounds % p.share;
+  if (first < 0) first += p.share;
+  const int64_t dst = layer * p.s_layer + blk * p.s_block + off * p.s_token + v0;
+  const uint4* const nk = p.new_k + layer * p.k_layer + b * p.k_batch + t * p.k_token + v0;
+  const uint4* const nv = p.new_v + layer * p.v_layer + b * p.v_batch + t * p.v_token + v0;
+  for (row = first * ROWS + sub; row < 2 * p.n_kv_heads; row += kRopeBatch * step) {
+#pragma unroll
+    for (int i = 0; i < kRopeBatch; ++i) {
+      const int h = row + i * step, g = h - p.n_kv_heads;
+      if (g < p.n_kv_heads) {
+        const uint4* const from = g < 0 ? nk + h * p.k_head : nv + g * p.v_head;
+        x[i] = from[0];
+        y[i] = from[dv];
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < kRopeBatch; ++i) {
+      const int h = row + i * step, g = h - p.n_kv_heads;
+      if (g < p.n_kv_heads) {
+        if (rotates && g < 0) turn_pairs<INTER>(x[i], y[i], c, s);
+        uint4* const into = g < 0 ? p.k + dst + h * p.s_head : p.v + dst + g * p.s_head;
+        into[0] = x[i];
+        into[dv] = y[i];
+      }
     }
   }
 }
 
 // ONE: the only CTA of the launch, which also counts the new tokens
 template <int D, bool INTER, bool ONE>
-__global__ void __launch_bounds__(ONE ? kRopeOneThreads : kRopeThreads) rope_append_kernel(const __grid_constant__ RopeParams p, uint32_t n_warps) {
+__global__ void __launch_bounds__(ONE ? kRopeOneThreads : kRopeThreads, ONE ? 1 : kRopeCtas) rope_append_kernel(const __grid_constant__ RopeParams p, uint32_t n_warps) {
   pdl_launch_next();
   pdl_wait();
   const uint32_t warp = blockIdx.x * (kRopeThreads / 32) + (threadIdx.x >> 5);
   if (warp < n_warps) rope_rows<D, INTER>(p, warp, threadIdx.x & 31);
   if constexpr (ONE) {
     __syncthreads();                               // every thread has read the lengths
-    for (int b = threadIdx.x; b < p.batch; b += blockDim.x) {
-      int start, n;
-      if (rope_range(p, b, start, n)) p.seq_lens[b] = start + n;
-    }
+    for (int b = threadIdx.x; b < p.batch; b += blockDim.x) rope_count(p, b);
   }
 }
 
@@ -159,8 +265,7 @@ __global__ void rope_count_kernel(const __grid_constant__ RopeParams p) {
   pdl_launch_next();
   pdl_wait();
   const int b = blockIdx.x * blockDim.x + threadIdx.x;
-  int start, n;
-  if (b < p.batch && rope_range(p, b, start, n)) p.seq_lens[b] = start + n;   // the append has reported the others
+  if (b < p.batch) rope_count(p, b);
 }
 
 static bool rows_ok(const specvlm_rows_t* r) {
@@ -236,7 +341,7 @@ extern "C" int32_t specvlm_rope_append_kv(const specvlm_kv_t* kv, const specvlm_
   c.seq_lens = seq_lens_inout;
   const int32_t rc = validate_kv(&c, batch, true);
   if (rc != SPECVLM_OK) return rc;
-  if (n_new > c.max_seq_len || !rope->turns || rope->n_axes < 1 || rope->n_axes > 3) return SPECVLM_ERR_INVALID_ARG;
+  if (n_new > c.max_seq_len || !rope->turns || !aligned16(rope->turns) || rope->n_axes < 1 || rope->n_axes > 3) return SPECVLM_ERR_INVALID_ARG;
   if (rope->rot_dim < 16 || rope->rot_dim > c.head_dim || rope->rot_dim % 16 != 0) return SPECVLM_ERR_UNSUPPORTED_SHAPE;
   if (!isfinite(rope->factor)) return SPECVLM_ERR_INVALID_ARG;
   int64_t pairs = 0;
@@ -273,15 +378,15 @@ extern "C" int32_t specvlm_rope_append_kv(const specvlm_kv_t* kv, const specvlm_
   p.n_layers = c.n_layers; p.batch = batch; p.n_new = n_new; p.n_q_heads = n_q_heads; p.n_kv_heads = c.n_kv_heads;
   p.n_rot = rope->rot_dim / 16;
   p.n_axes = rope->n_axes;
-  p.axis1 = rope->n_axes > 1 ? rope->sections[0] : 0;
-  p.axis2 = rope->n_axes > 1 ? rope->sections[0] + rope->sections[1] : 0;
+  p.axis1 = rope->n_axes > 1 ? rope->sections[0] : rope->rot_dim;
+  p.axis2 = rope->n_axes > 1 ? rope->sections[0] + rope->sections[1] : rope->rot_dim;
   p.counted = counted ? 1 : 0;
   p.factor = rope->factor;
   const int64_t tokens = (int64_t)c.n_layers * batch * n_new;
-  const int64_t n_rows = (int64_t)n_q_heads + 2 * (int64_t)c.n_kv_heads, rows = 32 / (c.head_dim / 16);
-  if (tokens > 0x3fffffff || n_rows > 65535) return SPECVLM_ERR_UNSUPPORTED_SHAPE;
+  const int64_t rows = 32 / (c.head_dim / 16);
+  if (tokens > 0x3fffffff || n_q_heads > 65535 || c.n_kv_heads > 65535) return SPECVLM_ERR_UNSUPPORTED_SHAPE;
   // a token's rows go to as many warps as it takes to occupy the SMs, up to a round each
-  const int64_t rounds = (n_rows + rows - 1) / rows, wanted = (int64_t)sm_count() * 32;
+  const int64_t rounds = (n_q_heads + rows - 1) / rows + (2 * c.n_kv_heads + rows - 1) / rows, wanted = (int64_t)sm_count() * kRopeWarps;
   int64_t share = (wanted + tokens - 1) / tokens;
   p.share = (int32_t)(share < rounds ? share : rounds);
   // few tokens that have to be counted: one CTA, which spares the second launch

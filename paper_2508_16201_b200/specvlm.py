@@ -256,6 +256,8 @@ class KvCache:
         self.k, self.v, self.seq_lens, self.block_table = k, v, seq_lens, block_table
         self.max_seq_len = int(max_seq_len)
         L, NB, H, BT, D = k.shape
+        self.dims = (L, H, D)
+        self.n_pages = NB
         s = KvStruct()
         s.k, s.v = k.data_ptr(), v.data_ptr()
         s.stride_layer, s.stride_block, s.stride_head, s.stride_token = (k.stride(0), k.stride(1),
@@ -345,7 +347,8 @@ def window_attn(kv: KvCache, q: torch.Tensor, window: int, n_sinks: int, sm_scal
     """q, out: bf16 [n_layers][batch][n_q][n_q_heads][head_dim]; a query sees the last ``window`` keys up to its own and the
     first ``n_sinks``."""
     L, B, NQ, Hq, D = q.shape
-    assert q.is_contiguous() and q.dtype == torch.bfloat16 and L == kv.n_layers and D == kv.head_dim
+    dims = kv.dims
+    assert q.is_contiguous() and q.dtype is torch.bfloat16 and L == dims[0] and D == dims[2]
     if out is None:
         out = torch.empty_like(q)
     if ws is None:
@@ -549,16 +552,19 @@ def rope_append_kv(kv: KvCache, rope: Rope, q: torch.Tensor | None, new_k: torch
     """q: bf16 [n_layers][batch][n_new][n_q_heads][head_dim] (None: keys only), new_k / new_v the same with the KV heads, all
     of any strides with a unit channel stride; returns the rotated queries.  kv.seq_lens is updated unless ``counted``, which
     says that it includes the new tokens already.  positions: int32 [n_axes][batch][n_new]."""
-    L, B, n, H, D = new_k.shape
-    assert new_k.dtype == torch.bfloat16 and new_v.dtype == torch.bfloat16 and new_v.shape == new_k.shape
-    assert L == kv.n_layers and H == kv.n_kv_heads and D == kv.head_dim
+    shape = new_k.shape
+    L, B, n, H, D = shape
+    bf16 = torch.bfloat16
+    assert new_k.dtype is bf16 and new_v.dtype is bf16 and new_v.shape == shape and (L, H, D) == kv.dims
     n_q_heads = 0
     if q is not None:
-        n_q_heads = q.shape[3]
-        assert q.dtype == torch.bfloat16 and q.shape == (L, B, n, n_q_heads, D)
+        q_shape = q.shape
+        n_q_heads = q_shape[3]
+        assert q.dtype is bf16 and q_shape == (L, B, n, n_q_heads, D)
         if q_out is None:
-            q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
-        assert q_out.dtype == torch.bfloat16 and q_out.shape == q.shape
+            q_out = torch.empty(q_shape, dtype=bf16, device=q.device)
+        else:
+            assert q_out.dtype is bf16 and q_out.shape == q_shape
     if positions is not None:
         assert positions.dtype == torch.int32 and positions.is_contiguous()
         assert positions.numel() == rope.struct.n_axes * B * n
@@ -579,9 +585,10 @@ def pages_workspace_bytes(kv: KvCache, batch: int) -> int:
 def _pages(kv: KvCache, ref_count: torch.Tensor) -> int:
     """Checks what the calls on pages share; returns the batch."""
     assert kv.block_table is not None, "a cache without a block table has no pages"
-    assert ref_count.dtype == torch.int32 and ref_count.is_contiguous() and ref_count.numel() == kv.k.shape[1]
-    assert kv.seq_lens.numel() >= kv.block_table.shape[0]
-    return kv.block_table.shape[0]
+    assert ref_count.dtype is torch.int32 and ref_count.is_contiguous() and ref_count.numel() == kv.n_pages
+    batch = kv.block_table.shape[0]
+    assert kv.seq_lens.numel() >= batch
+    return batch
 
 
 def reserve_pages(kv: KvCache, ref_count: torch.Tensor, n_new: int = 0, new_lens: torch.Tensor | None = None,
