@@ -56,7 +56,7 @@ struct Rows16 {
 
   // tile0: position of the tile's first token; vt: the V tile (generic address); cw: this warp's 16-token slice
   template <bool WIN, typename P>
-  __device__ __forceinline__ void tile(const P& p, uint32_t k_base, uint32_t v_base, uint8_t* vt, int tile0, const KeyView& view,
+  __device__ __forceinline__ void tile(const P& p, int n_q, uint32_t k_base, uint32_t v_base, uint8_t* vt, int tile0, const KeyView& view,
                                        int cw, int lane) {
     const int kv_len = view.len;
     const float scale_log2 = p.scale_log2;
@@ -106,16 +106,28 @@ struct Rows16 {
     }
     // scale, causal / length mask, running max
     float mx0 = -INFINITY, mx1 = -INFINITY;
+    // (WIN: most slices lie inside every query's window; rows out of use may then hold anything)
+    if (WIN && tb + 16 <= view.len - n_q + 1 && (tb >= view.lo + n_q - 1 || tb + 16 <= p.n_sinks)) {
 #pragma unroll
-    for (int nt = 0; nt < 2; ++nt) {
+      for (int nt = 0; nt < 2; ++nt) {
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const int tok = tb + nt * 8 + col + (e & 1);
-        const int lim = (e < 2) ? lim0 : lim1;
-        const bool seen = tok < lim && (!WIN || tok >= lim - p.window || tok < p.n_sinks);
-        const float v = seen ? sc[nt][e] * scale_log2 : -INFINITY;
-        sc[nt][e] = v;
-        if (e < 2) mx0 = fmaxf(mx0, v); else mx1 = fmaxf(mx1, v);
+        for (int e = 0; e < 4; ++e) {
+          sc[nt][e] *= scale_log2;
+          if (e < 2) mx0 = fmaxf(mx0, sc[nt][e]); else mx1 = fmaxf(mx1, sc[nt][e]);
+        }
+      }
+    } else {
+#pragma unroll
+      for (int nt = 0; nt < 2; ++nt) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const int tok = tb + nt * 8 + col + (e & 1);
+          const int lim = (e < 2) ? lim0 : lim1;
+          const bool seen = tok < lim && (!WIN || tok >= lim - p.window || tok < p.n_sinks);
+          const float v = seen ? sc[nt][e] * scale_log2 : -INFINITY;
+          sc[nt][e] = v;
+          if (e < 2) mx0 = fmaxf(mx0, v); else mx1 = fmaxf(mx1, v);
+        }
       }
     }
     mx0 = fmaxf(mx0, __shfl_xor_sync(0xffffffffu, mx0, 1));
@@ -300,7 +312,7 @@ __device__ __forceinline__ void rows16_consume(const AttnParams& p, uint8_t* sme
       break;
     }
     const uint32_t k_base = base + s * STAGE_BYTES;
-    st.template tile<WIN>(p, k_base, k_base + TILE_BYTES, smem + s * STAGE_BYTES + TILE_BYTES, (i * n_cta + rank) * kTileTokens, view,
+    st.template tile<WIN>(p, p.n_q, k_base, k_base + TILE_BYTES, smem + s * STAGE_BYTES + TILE_BYTES, (i * n_cta + rank) * kTileTokens, view,
                           cw, lane);
     __syncwarp();
     if (lane == 0) mbar_arrive(bar_empty + 8 * s);
@@ -398,9 +410,10 @@ __device__ __forceinline__ void rows16_consume(const AttnParams& p, uint8_t* sme
 constexpr int kSoloTiles = 4, kSoloTilesPair = 6;
 // (CTAs per SM are as many as the ring allows; without that the compiler held d = 64 to 96 registers and spilled: 6 layers of
 // 800 tokens, 24 items, 4.4 -> 4.2 us, 112 items of d = 128 and 755 tokens 9.83 -> 9.65)
+constexpr int kHalfRing = 4;      // stages of a CTA with two groups that shares an SM with another (d = 64)
 // WIN: queries see a window and sinks (KeyView); the first tile is not known before the length then.
 template <int D, int STAGES, int NG, bool SPLIT, bool WIN = false>
-__global__ void __launch_bounds__(32 * (4 * NG + 1), NG == 2 ? 1 : D == 64 ? 4 : 2)
+__global__ void __launch_bounds__(32 * (4 * NG + 1), NG == 2 ? (STAGES == kHalfRing ? 2 : 1) : D == 64 ? 4 : 2)
 attn_rows16_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v,
                    const AttnParams p) {
   constexpr int TILE_BYTES = kTileTokens * D * 2;
@@ -688,7 +701,7 @@ attn_rows16_slices_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid
         break;
       }
       const uint32_t k_base = base + s * STAGE_BYTES;
-      st.template tile<WIN>(p, k_base, k_base + TILE_BYTES, smem + s * STAGE_BYTES + TILE_BYTES, (sg.tile0 + j) * kTileTokens, view,
+      st.template tile<WIN>(p, p.n_win, k_base, k_base + TILE_BYTES, smem + s * STAGE_BYTES + TILE_BYTES, (sg.tile0 + j) * kTileTokens, view,
                             cw, lane);
       __syncwarp();
       if (lane == 0) mbar_arrive(bar_empty + 8 * s);
@@ -852,6 +865,9 @@ static int32_t launch_rows16(const CUtensorMap& tk, const CUtensorMap& tv, const
   const int64_t ctas = (int64_t)grid.x * grid.y * grid.z;
   constexpr int kDeep = D == 128 ? 6 : 12;
   if (grid.x > 1) return launch_rows16_s<D, kDeep, 2, true, WIN>(tk, tv, p, grid, st);
+  // Short windows, two CTAs an SM: their tiles, one after the other, are the time, and two groups halve them.
+  if constexpr (WIN && D == 64)
+    if (ctas > sm_count() && ctas <= 2 * sm_count()) return launch_rows16_s<D, kHalfRing, 2, false, WIN>(tk, tv, p, grid, st);
   return ctas <= sm_count() ? launch_rows16_s<D, kDeep, 2, false, WIN>(tk, tv, p, grid, st)
                             : launch_rows16_s<D, 3, 1, false, WIN>(tk, tv, p, grid, st);
 }
