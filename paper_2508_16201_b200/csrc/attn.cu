@@ -238,16 +238,6 @@ __device__ __forceinline__ void store_bf16x4(__nv_bfloat16* dst, const float4& v
 }
 
 constexpr int kMaxRows16Cluster = 8;       // the portable cluster size
-__device__ __forceinline__ float ld_cluster_f32(uint32_t addr) {
-  float v;
-  asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(addr) : "memory");
-  return v;
-}
-__device__ __forceinline__ float4 ld_cluster_f32x4(uint32_t addr) {
-  float4 v;
-  asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(addr) : "memory");
-  return v;
-}
 
 // By a consumer thread of a CTA that gives up (a wait expired): it stays, bounded, until the producer has gone and the last
 // copies that it asked for have landed, since the CTA must not end under copies to its shared memory.  flags[0] is the abort

@@ -63,11 +63,39 @@ struct TcCfg {
   static_assert(SMALL + BIG <= kMaxSmem, "shared-memory plan does not fit");
 };
 
+constexpr int kMaxTcCluster = 8;            // the portable cluster size
+// First tile of a cluster's CTA
+__device__ __forceinline__ int cluster_tile(int rank, int tiles, int n_cta) { return (int)((uint32_t)rank * (uint32_t)tiles / (uint32_t)n_cta); }
+
+// The plan of a CTA of a cluster, by one thread: one segment, counted from its item's first tile.
+template <bool WIN>
+__device__ __forceinline__ void plan_cluster(const AttnTcParams& p, CtaSlice* out) {
+  const int item = (int)blockIdx.x / p.n_cluster, rank = (int)blockIdx.x - item * p.n_cluster;
+  Segment s;
+  const int lb = item / p.n_kv_heads;
+  s.layer = lb / p.batch;
+  s.b = lb - s.layer * p.batch;
+  s.g = item - lb * p.n_kv_heads;
+  s.item = item;
+  s.item_tiles = (key_view<WIN>(p, p.n_win, s.b).len + kBigTokens - 1) / kBigTokens;
+  s.tile0 = cluster_tile(rank, s.item_tiles, p.n_cluster);
+  s.n_tiles = cluster_tile(rank + 1, s.item_tiles, p.n_cluster) - s.tile0;
+  s.item_begin = 0;
+  out->total = s.item_tiles;
+  out->begin = s.tile0;
+  out->end = s.tile0 + s.n_tiles;
+  out->first = s;
+  out->n_active = out->parts = p.n_cluster;
+  out->any_empty = s.item_tiles == 0 && rank == 0;
+}
+
 // TREE: the window's visibility comes from per-token ancestor masks instead of the chain rule.
 // A template parameter, not a run-time branch: the chain kernel's code is untouched by the tree
 // variant (the softmax loop's speed proved sensitive to what is compiled around it).
-// WIN: a chain whose queries see a window and sinks (KeyView).
-template <int D, int M, bool TREE, bool WIN = false>
+// WIN: a chain whose queries see a window and sinks (KeyView).  CLUSTER: a cluster of p.n_cluster CTAs per (layer, sequence, KV
+// head), each with an equal part of its tiles; their results meet over distributed shared memory, each CTA folding its share
+// of the output positions, instead of in a second kernel.
+template <int D, int M, bool TREE, bool WIN = false, bool CLUSTER = false>
 __global__ void __launch_bounds__(kTcThreads, 1)
 attn_tc_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v,
                const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ AttnTcParams p) {
@@ -75,6 +103,8 @@ attn_tc_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__
   constexpr int SUB_BYTES = C::SUB_BYTES, NKP = C::NKP, NVP = C::NVP, NQ = C::NQ;
   constexpr int Q_BYTES = C::Q_BYTES, P_BYTES = C::P_BYTES;
   constexpr int NH = M / 64;                          // 16-lane halves a softmax warp may own
+  constexpr int kPartPitch = D + 8;                   // CLUSTER: floats of a row of a CTA's result
+  static_assert(!CLUSTER || M * kPartPitch * 4 <= C::OFF_Q, "a CTA's result does not fit the tiles' place");
   constexpr uint32_t kIdescQK = umma_idesc_bf16(M, kBigTokens, false, false);
   constexpr uint32_t kIdescPV = umma_idesc_bf16(M, D, false, true);   // V tile: channels run along the row
 
@@ -107,7 +137,7 @@ attn_tc_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__
   if (big + C::BIG > raw_addr + C::TOTAL) {
     pdl_wait();
     if (tid == 0) {
-      p.ws_cut[blockIdx.x] = make_int4(0, 0, 0, 0);
+      if (!CLUSTER) p.ws_cut[blockIdx.x] = make_int4(0, 0, 0, 0);
       if (p.d_status) *p.d_status = SPECVLM_ERR_CUDA;
     }
     return;
@@ -157,8 +187,12 @@ attn_tc_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__
     fence_proxy_async();
   }
   pdl_wait();
-  if (warp == 3) unwritten_parts(p, blockIdx.x, D, lane, 32);
-  if (warp == 0) plan_slice<kBigTokens, WIN>(p, prefix, slice, blockIdx.x, gridDim.x, lane);
+  if constexpr (CLUSTER) {
+    if (tid == 0) plan_cluster<WIN>(p, slice);
+  } else {
+    if (warp == 3) unwritten_parts(p, blockIdx.x, D, lane, 32);
+    if (warp == 0) plan_slice<kBigTokens, WIN>(p, prefix, slice, blockIdx.x, gridDim.x, lane);
+  }
   tc_fence_before_sync();
   __syncthreads();
   tc_fence_after_sync();
@@ -257,7 +291,7 @@ attn_tc_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__
   } else if (warp == 1) {
     // ================================================================ S = Q K^T issuer
     setmaxnreg_dec<kRegsLight>();
-    if (lane == 0) publish_cut_item(p, *slice, cta, cta, prefix);
+    if (!CLUSTER && lane == 0) publish_cut_item(p, *slice, cta, cta, prefix);
     if (active) {
       const bool leader = elect_one();
       SliceCursor c;
@@ -382,9 +416,9 @@ attn_tc_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__
 
     // sequences without any token: their outputs are zero, their LSE -inf
     if (slice->any_empty) {
-      for (int item = cta; item < n_items; item += (int)gridDim.x) {
+      for (int item = CLUSTER ? slice->first.item : cta; item < n_items; item += CLUSTER ? n_items : (int)gridDim.x) {
         const int lb = item / hkv, g = item - lb * hkv, b = lb % p.batch;
-        if (prefix[b + 1] != prefix[b]) continue;
+        if (!CLUSTER && prefix[b + 1] != prefix[b]) continue;
         if constexpr (TREE) check_tree(p.parents + (size_t)b * p.n_win, p.n_win, lane, p.d_status);
         for (int idx = st; idx < rows * (D / 8); idx += 256) {
           const int r = idx / (D / 8), c8 = idx - r * (D / 8);
@@ -765,7 +799,14 @@ attn_tc_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__
                 if (has1) acc += __uint_as_float(ob[k]) * w1[e];
                 res[2 * jj + x] = acc;
               }
-            if (complete) {
+            if constexpr (CLUSTER) {
+              // to this CTA's shared memory, where its K and V tiles were (every product of the item is complete)
+              float* dst = reinterpret_cast<float*>(big_ptr + C::OFF_K) + r * kPartPitch + cc * 64 + lc;
+#pragma unroll
+              for (int jj = 0; jj < 8; ++jj)
+                *reinterpret_cast<float2*>(dst + jj * 8) = make_float2(res[2 * jj], res[2 * jj + 1]);
+              if ((lane & 3) == 0 && cc == 0) reinterpret_cast<float*>(big_ptr + C::OFF_Q)[r] = lse2[e];
+            } else if (complete) {
               const int t = r / p.group, hq = sg.g * p.group + (r - t * p.group);
               const size_t orow = ((size_t)lb * p.n_win + t) * p.n_q_heads + hq;
               __nv_bfloat16* dst = p.out + orow * D + cc * 64 + lc;
@@ -793,6 +834,66 @@ attn_tc_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__
   softmax_done:
     if (!ok && p.d_status && gt == 0) *p.d_status = SPECVLM_ERR_TIMEOUT;
 #undef SM_WAIT
+    if constexpr (CLUSTER) {
+      // A CTA's result counts where it has tiles; if a wait expired in any CTA the item is left alone.
+      const int n_cta = p.n_cluster, rank = (int)blockIdx.x % n_cta;
+      if (!active && st < rows) reinterpret_cast<float*>(big_ptr + C::OFF_Q)[st] = -INFINITY;      // a CTA without a tile
+      cluster_barrier();                                    // every role of every CTA has ended
+      if (slice->first.item_tiles > 0) {
+        const uint32_t part_o = smem_u32(big_ptr + C::OFF_K), part_lse = smem_u32(big_ptr + C::OFF_Q);
+        const int lb = slice->first.layer * p.batch + slice->first.b, g = slice->first.g;
+        const uint32_t flag = smem_u32(const_cast<int*>(abort_flag));
+        for (int idx = rank * 256 + st; idx < rows * (D / 4); idx += n_cta * 256) {
+          const int r = idx / (D / 4), c4 = idx - r * (D / 4);
+          float lse[kMaxTcCluster], flags[kMaxTcCluster];
+          float4 x[kMaxTcCluster];
+#pragma unroll
+          for (int k = 0; k < kMaxTcCluster; ++k) {
+            lse[k] = -INFINITY;
+            flags[k] = 0.f;
+            if (k < n_cta) {
+              flags[k] = ld_cluster_f32(cluster_map(flag, k));
+              lse[k] = ld_cluster_f32(cluster_map(part_lse + 4 * r, k));
+              x[k] = ld_cluster_f32x4(cluster_map(part_o + (r * kPartPitch + c4 * 4) * 4, k));
+            }
+          }
+          float mm = -INFINITY, den = 0.f;
+          bool lost = false;
+#pragma unroll
+          for (int k = 0; k < kMaxTcCluster; ++k) {
+            lost |= __float_as_int(flags[k]) != 0;
+            mm = fmaxf(mm, lse[k]);
+          }
+          if (lost) continue;
+          float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+          for (int k = 0; k < kMaxTcCluster; ++k) {
+            if (lse[k] == -INFINITY) continue;              // nothing there: not even a zero
+            const float w = fast_exp2(lse[k] - mm);
+            acc.x += w * x[k].x;
+            acc.y += w * x[k].y;
+            acc.z += w * x[k].z;
+            acc.w += w * x[k].w;
+            den += w;
+          }
+          const float inv = den > 0.f ? 1.f / den : 0.f;
+          const int t = r / p.group, h = g * p.group + (r - t * p.group);
+          const size_t orow = ((size_t)lb * p.n_win + t) * p.n_q_heads + h;
+          uint2 packed;
+          packed.x = pack_bf16x2(acc.x * inv, acc.y * inv);
+          packed.y = pack_bf16x2(acc.z * inv, acc.w * inv);
+          *reinterpret_cast<uint2*>(p.out + orow * D + c4 * 4) = packed;
+          if (p.lse && c4 == 0) p.lse[orow] = den > 0.f ? (mm + log2f(den)) * kLn2 : -INFINITY;
+        }
+      }
+      cluster_barrier_relaxed();                            // nobody reads this CTA's shared memory any more
+    }
+  }
+  if constexpr (CLUSTER) {
+    if (warp < 4) {                                         // the other roles' part in the two barriers above
+      cluster_barrier();
+      cluster_barrier_relaxed();
+    }
   }
 
   // every role ends here; the allocating warp returns the tensor memory
@@ -1012,6 +1113,30 @@ size_t attn_tc_ws_bytes(const specvlm_kv_t* kv, int32_t batch, int rows, int gro
   return tc_scratch(kv, pl, group).bytes();
 }
 
+// CTAs per item of a call with a window, whose items are all about as long: a cluster each (of one CTA, too), or 0 for slices and
+// their merge.  A cluster costs 7.8 us around its CTAs' tiles, which take 0.7 to 1.3 us each, or around the bytes; slices 12.3
+// (18 with more than 64 rows) around the bytes, with the merge kernel.  As many clusters as run side by side: 12 of eight CTAs do and 16 do not, 32 of
+// four and not 36, 72 of two.  Measured, 6 tokens of 8 heads per KV head at d = 128, cluster / slices: 8 items of 512 keys 8.6 /
+// 11.3 us, of 4096 12.7 / 14.9, of 16 384 24.6 / 22.7; 32 of 1024 12.5 / 18.8, of 4096 19.5 / 25.9; 64 of 4096 29.1 / 34.4; 96 of
+// 1024 19.8 / 24.6; 144 of 1024 22.7 / 22.5; 128 rows, 16 of 4096 21.4 / 25.5.  (The flags of the CTAs that gave up in the
+// LSEs, behind one more barrier of the CTA, instead of beside them: 0.4 us more with eight.)
+static int tc_cluster(const specvlm_kv_t* kv, int64_t items, int rows) {
+  const int64_t tiles = (kv->max_seq_len + kBigTokens - 1) / kBigTokens;
+  const double tile_us = kv->head_dim == 128 ? (rows > 64 ? 1.3 : 0.93) : (rows > 64 ? 1.0 : 0.7);
+  const double hbm_us = (double)items * kv->max_seq_len * (4.0 * kv->head_dim) / 6.5e6;
+  int best = 0;
+  double best_us = (rows > 64 ? 18.0 : 12.3) + hbm_us;
+  for (int n = 1; n <= kMaxTcCluster; n *= 2) {
+    const int fit = n == 1 ? sm_count() : n == 2 ? 72 : n == 4 ? 32 : 12;
+    const double own_us = tile_us * (double)((tiles + n - 1) / n), us = 7.8 + (own_us > hbm_us ? own_us : hbm_us);
+    if (items <= fit && us < best_us) {
+      best = n;
+      best_us = us;
+    }
+  }
+  return best;
+}
+
 // Queries as a 5-D tensor (channel, head in group, query token, KV head, layer * batch + sequence):
 // the box (64 channels, group, n_q, 1, 1) at token q0 is one item's rows of a launch, r = t * group + head.
 static int32_t encode_q_map(CUtensorMap* map, const void* q, int D, int group, int n_win, int n_q, int n_kv_heads,
@@ -1056,6 +1181,8 @@ template <int D, int M>
 static int32_t launch_tc(const CUtensorMap& tk, const CUtensorMap& tv, const CUtensorMap& tq, const AttnTcParams& p,
                          int grid, cudaStream_t st) {
   constexpr int kSmem = TcCfg<D, M>::TOTAL;
+  if (p.n_cluster > 0)
+    return launch_tc_kernel<attn_tc_kernel<D, M, false, true, true>>(kSmem, tk, tv, tq, p, grid, st, p.n_cluster);
   if (p.window > 0) return launch_tc_kernel<attn_tc_kernel<D, M, false, true>>(kSmem, tk, tv, tq, p, grid, st);
   return p.parents ? launch_tc_kernel<attn_tc_kernel<D, M, true>>(kSmem, tk, tv, tq, p, grid, st)
                : launch_tc_kernel<attn_tc_kernel<D, M, false>>(kSmem, tk, tv, tq, p, grid, st);
@@ -1081,7 +1208,8 @@ int32_t attn_tc_launch(const specvlm_kv_t* kv, const void* q, int32_t batch, int
   if (ws_bytes < attn_tc_ws_bytes(&sched, batch, rows, group)) return SPECVLM_ERR_WORKSPACE_TOO_SMALL;
   if (tree_parents && n_q > kMaxTreeNodes) return SPECVLM_ERR_UNSUPPORTED_SHAPE;
   if (pl.q_per * group > 128) return SPECVLM_ERR_UNSUPPORTED_SHAPE;
-  const int ctas = pl.ctas, n_parts = pl.n_parts;
+  const int n_parts = pl.n_parts, cluster = win ? tc_cluster(&sched, items, rows) : 0;
+  const int ctas = cluster > 0 ? (int)items * cluster : pl.ctas;
 
   CUtensorMap tk, tv;
   int32_t rc = encode_kv_map(&tk, kv, kv->k, kTileTokens);
@@ -1094,6 +1222,7 @@ int32_t attn_tc_launch(const specvlm_kv_t* kv, const void* q, int32_t batch, int
   if (win) {
     p.window = win->window;
     p.n_sinks = win->n_sinks;
+    p.n_cluster = cluster;
     if (n_parts > 1) return SPECVLM_ERR_UNSUPPORTED_SHAPE;
   }
 
@@ -1106,7 +1235,7 @@ int32_t attn_tc_launch(const specvlm_kv_t* kv, const void* q, int32_t batch, int
     rc = p.rows <= 64 ? launch_tc<128, 64>(tk, tv, tq, p, ctas, st) : launch_tc<128, 128>(tk, tv, tq, p, ctas, st);
   else
     rc = p.rows <= 64 ? launch_tc<64, 64>(tk, tv, tq, p, ctas, st) : launch_tc<64, 128>(tk, tv, tq, p, ctas, st);
-  if (rc != SPECVLM_OK) return rc;
+  if (rc != SPECVLM_OK || cluster > 0) return rc;
   return attn_merge_launch(p, kv->head_dim, ctas, st);
 }
 

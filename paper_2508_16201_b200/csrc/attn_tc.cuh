@@ -30,6 +30,7 @@ struct AttnTcParams {
   int32_t lost_cta;           // test hook (attn.cu): the CTA that gives up as if a wait had expired; -1 as a rule
   int32_t window, n_sinks;    // specvlm_window_attn: the last keys and the first keys that a query sees
   int32_t n_blocks;           // pages of the cache
+  int32_t n_cluster;          // CTAs of a cluster, which share an item (attn_tc.cu); 0: slices
 };
 
 constexpr float kRescaleThreshold = 8.f;   // log2 units
@@ -384,6 +385,7 @@ inline AttnTcParams slice_params(const specvlm_kv_t* kv, const void* q, int32_t 
   p.lost_cta = -1;
   p.window = p.n_sinks = 0;
   p.n_blocks = kv->n_blocks;
+  p.n_cluster = 0;
   return p;
 }
 
@@ -410,7 +412,7 @@ SlicePlan attn_tc_plan(const specvlm_kv_t* kv, int32_t batch, int32_t group, int
 // (a template of the kernel itself: kernels of one signature must not share the flag below)
 template <auto kern>
 static int32_t launch_tc_kernel(int smem, const CUtensorMap& tk, const CUtensorMap& tv, const CUtensorMap& tq,
-                                const AttnTcParams& p, int grid, cudaStream_t st) {
+                                const AttnTcParams& p, int grid, cudaStream_t st, int cluster = 1) {
   // once per device and kernel: the opt-in shared-memory size, and the check that the compiled
   // kernel's register pool can satisfy the setmaxnreg requests (it never changes)
   static std::atomic<uint64_t> attr_done{0};
@@ -422,7 +424,7 @@ static int32_t launch_tc_kernel(int smem, const CUtensorMap& tk, const CUtensorM
     if (fa.numRegs * kTcThreads < kRegsNeeded) return SPECVLM_ERR_CUDA;   // setmaxnreg could never be satisfied
     if (!smem_attr_once(attr_done, reinterpret_cast<const void*>(kern), smem)) return SPECVLM_ERR_CUDA;
   }
-  return launch_after(kern, dim3((unsigned)grid), dim3(kTcThreads), (size_t)smem, st, tk, tv, tq, p);
+  return launch_clusters_after(kern, dim3((unsigned)grid), cluster, dim3(kTcThreads), (size_t)smem, st, tk, tv, tq, p);
 }
 
 }  // namespace specvlm

@@ -148,6 +148,15 @@ def test_larger_calls(L, B, Hq, H, D, n_q, window, sinks, page):
     _run(L, Hq, H, D, n_q, [5000 - 97 * (b % 20) for b in range(B)], window, sinks, page=page, seed=L + B)
 
 
+@pytest.mark.parametrize("L,B,H", [(1, 2, 1), (1, 3, 4), (1, 5, 4), (2, 8, 2), (3, 11, 2), (1, 20, 5), (4, 20, 2)])
+@pytest.mark.parametrize("Hq,D,n_q", [(4, 128, 6), (4, 64, 9), (16, 128, 8), (13, 64, 7)])
+def test_items_of_every_number(L, B, H, Hq, D, n_q):
+    """From two items to 160: clusters of eight, four, two and one CTAs, and slices; sequences shorter than a cluster's tiles and
+    empty ones among them."""
+    lens = [[700, 0, 1, 129, 350, 64, 900][(b * 3 + b // 7) % 7] for b in range(B)]
+    _run(L, Hq * H, H, D, n_q, lens, 260, 70, page=64, seed=B)
+
+
 def test_a_roomy_cache_and_mapped_pages():
     """Room behind the longest sequence; pages out of the window still mapped."""
     _run(2, 8, 1, 128, 1, [100, 400], 90, 5, page=0, seed=2, extra=5000)
