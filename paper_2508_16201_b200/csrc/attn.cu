@@ -742,18 +742,20 @@ static double rows16_tile_us(const specvlm_kv_t* kv) {
   return (kv->head_dim == 128 ? 0.35 : 0.25) * (kv->block_table ? 1.25 : 1.0);
 }
 
+// (window: a call with a window, whose items are all as long as the host's bound.  There 32 clusters of four and 12 of eight, which
+// do run side by side, are used too: 32 items, d = 128, window 512 / 1024 6.53 / 8.45 -> 6.01 / 7.35 us, 12 of 1024 6.56 -> 5.85.)
 // CTAs per item of a launch without slices: the number that is the fastest where every CTA has an SM of its own.  The
 // hand-over costs 1.3 us: one layer of 4 items of 200 tokens 3.7 us with a CTA each, 4.3 with two; of 800 / 1600 / 3200
 // tokens 7.0 / 11.3 / 20.1 with one (7.4 / 8.5 on slices from 1600) and 4.4 / 5.0 / 6.3 with eight.  Clusters do not use
 // every SM of a GPC: 16 of eight CTAs no longer run side by side (4 layers of 800 tokens 7.3 -> 8.4), 24 of four do (2 layers
 // x 3 sequences of 800 tokens 8.0 -> 5.4).
-static int rows16_cluster(const specvlm_kv_t* kv, int64_t items, int64_t tiles) {
+static int rows16_cluster(const specvlm_kv_t* kv, int64_t items, int64_t tiles, bool window = false) {
   if (g_forced_splits.load(std::memory_order_relaxed) == 1) return 1;
   int best = 1;
   double best_us = rows16_tile_us(kv) * tiles;
   for (int n = 2; n <= kMaxRows16Cluster; n *= 2) {
     const double us = 1.3 + rows16_tile_us(kv) * ((tiles + n - 1) / n);
-    if (items * n <= (n == 2 ? 144 : n == 4 ? 96 : 64) && us < best_us) {
+    if (items * n <= (n == 2 ? 144 : n == 4 ? (window ? 128 : 96) : (window ? 96 : 64)) && us < best_us) {
       best = n;
       best_us = us;
     }
@@ -762,7 +764,7 @@ static int rows16_cluster(const specvlm_kv_t* kv, int64_t items, int64_t tiles) 
 }
 
 // Whether slices are worth a workspace: estimated times in us, from the host's bound on the lengths, against a CTA per item.
-static bool rows16_slices_beat_ctas(const specvlm_kv_t* kv, int32_t batch, int64_t items, int64_t tiles) {
+static bool rows16_slices_beat_ctas(const specvlm_kv_t* kv, int32_t batch, int64_t items, int64_t tiles, bool window) {
   // A CTA per item: about 3 us around the tiles; while the items fit the SMs the longest one counts (one CTA takes 0.35 us
   // a tile at d = 128, a quarter more with a block table) or HBM does; beyond, rounds of two CTAs per SM at 0.75 us a tile,
   // or HBM with a last round that is partly empty.  Slices: 4.5 us with the merge kernel, the bytes, 2 us for every
@@ -774,7 +776,7 @@ static bool rows16_slices_beat_ctas(const specvlm_kv_t* kv, int32_t batch, int64
   // 18.1 / 34.0 against 28.1 / 41.4.
   const int64_t sms = sm_count();
   const double hbm = (double)items * tiles * (256.0 * kv->head_dim) / 6.65e6;
-  const double ragged = batch > 1 ? 0.85 : 1.0;
+  const double ragged = batch > 1 && !window ? 0.85 : 1.0;
   double per_item;
   if (items <= sms) {
     const double longest = rows16_tile_us(kv) * tiles;
@@ -790,7 +792,7 @@ static bool rows16_slices_beat_ctas(const specvlm_kv_t* kv, int32_t batch, int64
 // CTAs of a launch on slices, or 0 for a CTA (or a cluster) per item.  *scratch_ctas: the CTAs that the workspace has to
 // have room for, 0 for none.  It does not depend on whether a cluster takes the slices' place: the choice between the two
 // turns back and forth with the length, and a workspace sized for the longest sequences has to serve the shorter ones.
-static int rows16_slices(const specvlm_kv_t* kv, int32_t batch, int* scratch_ctas) {
+static int rows16_slices(const specvlm_kv_t* kv, int32_t batch, int* scratch_ctas, bool window = false) {
   const int64_t items = (int64_t)kv->n_layers * batch * kv->n_kv_heads;
   const int64_t tiles = (kv->max_seq_len + kTileTokens - 1) / kTileTokens, sms = sm_count();
   const int forced = g_forced_splits.load(std::memory_order_relaxed);
@@ -800,9 +802,9 @@ static int rows16_slices(const specvlm_kv_t* kv, int32_t batch, int* scratch_cta
     const int64_t n = items * (forced < tiles ? forced : tiles);
     return *scratch_ctas = (int)(n < 4 * sms ? n : 4 * sms);
   }
-  if (!rows16_slices_beat_ctas(kv, batch, items, tiles)) return 0;
+  if (!rows16_slices_beat_ctas(kv, batch, items, tiles, window)) return 0;
   *scratch_ctas = sched_scratch_ctas(items * tiles, (int)sms);
-  const int n = rows16_cluster(kv, items, tiles);
+  const int n = rows16_cluster(kv, items, tiles, window);
   if (n > 1) {
     // A cluster per item, 3.9 us around its CTAs' tiles or the bytes, which half the SMs do not stream as well, against
     // slices, 6.5 us around the bytes (in pages 6) and more for many parts an item.  Measured, cluster / slices: 1 item
@@ -810,7 +812,7 @@ static int rows16_slices(const specvlm_kv_t* kv, int32_t batch, int* scratch_cta
     // 10 240 8.3 / 13.4 / 23.9 against 9.0 / 10.8 / 15.7; 40 of 2560 / 10 240 / 20 480 11.3 / 38.8 / 75.5 against 14.2 / 37.3 /
     // 64.7; 64 of 1280 / 2560 / 5120 / 10 240 7.5 / 15.3 / 28.4 / 52.6 against 11.0 / 20.5 / 31.8 / 55.0; 72 ragged ones of up to
     // 1280 / 2560 / 10 240 7.5 / 11.3 / 47.2 against 12.9 / 16.1 / 48.3.
-    const double hbm = (double)items * tiles * (256.0 * kv->head_dim) / 6.65e6, ragged = batch > 1 ? 0.85 : 1.0;
+    const double hbm = (double)items * tiles * (256.0 * kv->head_dim) / 6.65e6, ragged = batch > 1 && !window ? 0.85 : 1.0;
     const double longest = 1.08 * rows16_tile_us(kv) * ((tiles + n - 1) / n);
     const double parts = (double)(items * tiles < sms ? items * tiles : sms) / items;
     if ((kv->block_table ? 6.0 : 6.5) + ragged * hbm + 0.04 * parts >= 3.9 + (longest > 1.09 * hbm ? longest : 1.09 * hbm)) return 0;
@@ -824,9 +826,9 @@ static int rows16_slices(const specvlm_kv_t* kv, int32_t batch, int* scratch_cta
 static size_t rows16_scratch_bytes(const specvlm_kv_t* kv, int scratch_ctas, int rows) {
   return scratch_ctas == 0 ? 256 : SliceScratch(scratch_ctas, rows, kv->head_dim).bytes();
 }
-static size_t rows16_ws_bytes(const specvlm_kv_t* kv, int32_t batch, int rows) {
+static size_t rows16_ws_bytes(const specvlm_kv_t* kv, int32_t batch, int rows, bool window = false) {
   int scratch_ctas;
-  rows16_slices(kv, batch, &scratch_ctas);
+  rows16_slices(kv, batch, &scratch_ctas, window);
   return rows16_scratch_bytes(kv, scratch_ctas, rows);
 }
 
@@ -903,7 +905,7 @@ static int32_t attn_common(const specvlm_kv_t* kv, const void* q, int32_t batch,
 
   const specvlm_kv_t sched = win ? win->view(kv, n_q) : *kv;
   int scratch_ctas;
-  const int ctas = rows16_slices(&sched, batch, &scratch_ctas);
+  const int ctas = rows16_slices(&sched, batch, &scratch_ctas, win != nullptr);
   if (scratch_ctas > 0) {
     if (!ws || (reinterpret_cast<uintptr_t>(ws) & 255u)) return SPECVLM_ERR_INVALID_ARG;
     if (ws_bytes < rows16_scratch_bytes(kv, scratch_ctas, rows)) return SPECVLM_ERR_WORKSPACE_TOO_SMALL;
@@ -945,7 +947,7 @@ static int32_t attn_common(const specvlm_kv_t* kv, const void* q, int32_t batch,
   p.n_sinks = win ? win->n_sinks : 0;
   p.n_blocks = kv->n_blocks;
 
-  const int n = rows16_cluster(&sched, lb64 * kv->n_kv_heads, (sched.max_seq_len + kTileTokens - 1) / kTileTokens);
+  const int n = rows16_cluster(&sched, lb64 * kv->n_kv_heads, (sched.max_seq_len + kTileTokens - 1) / kTileTokens, win != nullptr);
   dim3 grid((unsigned)n, (unsigned)kv->n_kv_heads, (unsigned)lb64);
   if (n_ctas) *n_ctas = (int32_t)(grid.x * grid.y * grid.z);
   if (win) return kv->head_dim == 128 ? launch_rows16<128, true>(tk, tv, p, grid, st) : launch_rows16<64, true>(tk, tv, p, grid, st);
@@ -1027,7 +1029,9 @@ extern "C" size_t specvlm_window_attn_workspace_bytes(const specvlm_kv_t* kv, in
   if (!kv || n_q < 1 || window < 1 || n_sinks < 0 || kv->n_kv_heads < 1 || kv->max_seq_len < 1) return 0;
   if ((int64_t)n_q_heads / kv->n_kv_heads * n_q > kWindowMaxRows) return 0;
   const specvlm_kv_t view = KeyWindow(kv, window, n_sinks).view(kv, n_q);
-  return specvlm_attn_workspace_bytes(&view, batch, n_q_heads, n_q - 1);
+  const size_t bytes = specvlm_attn_workspace_bytes(&view, batch, n_q_heads, n_q - 1);      // 0: refused
+  const int rows = bytes > 0 ? n_q_heads / kv->n_kv_heads * n_q : 0;
+  return rows > 0 && rows <= kRows16Max ? rows16_ws_bytes(&view, batch, rows, true) : bytes;
 }
 
 extern "C" int32_t specvlm_window_attn(const specvlm_kv_t* kv, const void* q, int32_t batch, int32_t n_q_heads, int32_t n_q,
