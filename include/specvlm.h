@@ -466,15 +466,17 @@ int32_t specvlm_rope_append_kv(const specvlm_kv_t* kv, const specvlm_rope_t* rop
  *   ref_count_inout     device int32 [n_blocks]; at the start of a program zeros, with every table entry -1
  *   block_table_inout   device int32 [batch][kv->max_blocks], takes kv->block_table's place
  *   ws                  device scratch, specvlm_pages_workspace_bytes(kv, batch)
- * The counts and the tables have to agree: every table whose rows hold pages of the pool takes part in its compaction.
+ * The counts and the tables have to agree: every table whose rows hold pages of the pool takes part in its compaction, and
+ * calls on one pool are ordered (one stream, or events between them).
  *
  * specvlm_reserve_pages makes the next positions of every sequence writable: kv->seq_lens[b] .. + new - 1, with new =
  * new_lens[b] or n_new.  Of the pages that these fall on, an unmapped one is taken from the free ones; one that other rows
  * hold too is replaced by a fresh one, into which the rows that the sequence has on it already are copied (K and V, all
  * layers and heads), except that of several sequences of the call that go on in one and the same page the last keeps it
- * if nobody else holds it.  Pages replaced here are not handed out in the same call.  All or nothing: with too few free pages nothing changes, and SPECVLM_ERR_NO_PAGES is stored to
- * d_status.  A sequence without room (more than kv->max_seq_len tokens), or with a length or number of new tokens out of
- * range, gets nothing, and SPECVLM_ERR_INVALID_ARG is stored; the others get theirs.
+ * if nobody else holds it.  Pages replaced here are not handed out in the same call.  All or nothing: with too few free
+ * pages nothing changes, and SPECVLM_ERR_NO_PAGES is stored to d_status.  A sequence without room (more than
+ * kv->max_seq_len tokens), or with a length or number of new tokens out of range, gets nothing, and
+ * SPECVLM_ERR_INVALID_ARG is stored; the others get theirs.
  *
  * specvlm_release_pages gives back the pages that hold no row that is still needed: those wholly behind the sequence's
  * end, and those whose rows are all older than the last `window` tokens and not among the first n_sinks (1 <= window;

@@ -34,7 +34,8 @@ __device__ __forceinline__ KeyView key_view(const P& p, int n_q, int b) {
   KeyView v;
   v.len = clamp_len(p.seq_lens[b], p.max_seq_len);
   if constexpr (WIN) {
-    v.lo = v.len - n_q - p.window + 1;                     // the host has clamped the window to the cache's length
+    const int behind = v.len - p.window;                   // (the host has clamped the window to the cache's length)
+    v.lo = (behind > -kTileTokens ? behind : -kTileTokens) - (n_q - 1);       // no lower than it takes to say "all"
     v.gap_at = (p.n_sinks + kTileTokens - 1) & ~(kTileTokens - 1);
     v.gap = v.lo > v.gap_at ? (v.lo & ~(kTileTokens - 1)) - v.gap_at : 0;
     v.len -= v.gap;

@@ -157,6 +157,21 @@ def test_items_of_every_number(L, B, H, Hq, D, n_q):
     _run(L, Hq * H, H, D, n_q, lens, 260, 70, page=64, seed=B)
 
 
+@pytest.mark.parametrize("seed", range(40))
+def test_random_windows(seed):
+    rng = np.random.default_rng(1000 + seed)
+    D = int(rng.choice([64, 128]))
+    group, n_q = int(rng.integers(1, 17)), int(rng.choice([1, 1, 1, 2, 5, 7, 9]))
+    if group * n_q > 128:
+        n_q = 128 // group
+    H, L, B = int(rng.choice([1, 1, 2, 3])), int(rng.integers(1, 5)), int(rng.integers(1, 9))
+    top = int(rng.choice([70, 300, 1500]))
+    lens = [int(rng.integers(0, top + 1)) for _ in range(B)]
+    window, sinks = int(np.exp(rng.uniform(0, 8))), int(rng.choice([0, 0, 1, 4, 63, 64, 65, int(rng.integers(0, 500))]))
+    _run(L, group * H, H, D, n_q, lens, window, sinks, page=int(rng.choice([0, 64, 128, 256])), seed=seed, splits=int(rng.choice([0, 0, 1, 5])),
+         extra=int(rng.choice([0, 100])))
+
+
 def test_a_roomy_cache_and_mapped_pages():
     """Room behind the longest sequence; pages out of the window still mapped."""
     _run(2, 8, 1, 128, 1, [100, 400], 90, 5, page=0, seed=2, extra=5000)
