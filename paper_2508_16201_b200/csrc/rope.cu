@@ -1,8 +1,12 @@
 // Rotary positions of new tokens' queries and keys, fused with the append of keys and values to the cache.
 //
-// Every row is read once and written once; per 16 channels there are 8 pairs to turn, 24 multiply-adds, against 64 bytes of
-// traffic.  A warp works on one token of one layer and walks its rows (query heads, key heads, value heads), a thread on
-// the same 16 channels of each, so that the 8 sines and cosines of a thread serve all of them.
+// Every row is read once and written once: a long prompt is bound by HBM (one layer of 4 x 6528 tokens, 64 + 8 heads of d = 128,
+// 744 MB in 122 us, 6.1 TB/s).  A warp works on one token of one layer and walks its rows (query heads, then key and
+// value heads), a thread on the same 16 channels of each, so that the 8 sines and cosines of a thread serve all of them.  A
+// short call is bound by the chain of a warp -- lengths, angles, then a round trip to memory for every two rounds of rows
+// -- so a token's rounds are dealt out to several warps, and each angle is computed by one lane of a warp and handed on through
+// shared memory: 28 layers x 16 sequences x 6 tokens (50 MB) 19.7 us with a warp a token and every thread its own angles, 12.8 now,
+// the counting kernel (1.3) included.
 //
 // Angles: a position times a frequency in radians loses the angle's digits to the whole turns (position 50 000 in fp32: 2e-3
 // radians).  Here frequencies are fractions of a turn in 64-bit fixed point, and position * fraction modulo 2^64 is the exact
@@ -116,12 +120,12 @@ __device__ __forceinline__ void turn_sincos(uint32_t turn, float& s, float& c) {
 
 constexpr int kRopeThreads = 128, kRopeOneThreads = 512, kRopeOneTokens = 8;
 constexpr int kRopeCtas = 8;                       // on an SM: 64 registers a thread
-constexpr int kRopeWarps = 16;                     // on an SM: with fewer tokens several warps share one
+constexpr int kRopeWarps = 48;                     // on an SM: with fewer tokens several warps share one
 constexpr int kRopeBatch = 2;         // rounds whose loads are in flight together
 
 // A warp's rounds are the query rows first and then the key and value rows; those of a token are dealt out to `share` warps.
 template <int D, bool INTER>
-__device__ __forceinline__ void rope_rows(const RopeParams& p, uint32_t warp, int lane) {
+__device__ __forceinline__ void rope_rows(const RopeParams& p, float* cs_sm, uint32_t warp, int lane) {
   constexpr int UNITS = D / 16, ROWS = 32 / UNITS;  // threads of a row, rows of a round
   const uint32_t token = warp / (uint32_t)p.share, lb = token / (uint32_t)p.n_new;
   const int part = (int)(warp - token * p.share), t = (int)(token - lb * p.n_new);
@@ -135,18 +139,17 @@ __device__ __forceinline__ void rope_rows(const RopeParams& p, uint32_t warp, in
   // is the number of round trips to memory one after the other.
   const int n_asked = p.new_lens ? p.new_lens[b] : p.n_new, len = p.seq_lens[b];
   int pos[3] = {0, 0, 0};
-  ulonglong2 turns[4];
-  if (rotates) {
-    if (p.positions) {
-      const int32_t* const at = p.positions + (size_t)b * p.n_new + t;
-      const size_t axis = (size_t)p.batch * p.n_new;
+  if (p.positions) {
+    const int32_t* const where = p.positions + (size_t)b * p.n_new + t;
+    const size_t axis = (size_t)p.batch * p.n_new;
 #pragma unroll
-      for (int a = 0; a < 3; ++a)
-        if (a < p.n_axes) pos[a] = at[a * axis];
-    }
-#pragma unroll
-    for (int e = 0; e < 4; ++e) turns[e] = reinterpret_cast<const ulonglong2*>(p.turns)[4 * u + e];
+    for (int a = 0; a < 3; ++a)
+      if (a < p.n_axes) pos[a] = where[a * axis];
   }
+  constexpr int PER_LANE = D / 64;                  // pairs of a lane: each angle is computed once a warp
+  uint64_t turns[PER_LANE];
+#pragma unroll
+  for (int e = 0; e < PER_LANE; ++e) turns[e] = lane + 32 * e < 8 * p.n_rot ? p.turns[lane + 32 * e] : 0;
   uint4 x[kRopeBatch], y[kRopeBatch];
   int row = part * ROWS + sub;
   const int64_t q_step = step * p.q_head;
@@ -176,22 +179,28 @@ __device__ __forceinline__ void rope_rows(const RopeParams& p, uint32_t warp, in
     stored = blk >= 0 && blk < p.n_blocks;
     if (!stored && lane == 0 && p.d_status) *p.d_status = SPECVLM_ERR_INVALID_ARG;
   }
+  if (!p.positions) pos[0] = pos[1] = pos[2] = at;
+#pragma unroll
+  for (int e = 0; e < PER_LANE; ++e) {
+    const int i = lane + 32 * e, where = i < p.axis1 ? pos[0] : i < p.axis2 ? pos[1] : pos[2];
+    float sn, cs;
+    turn_sincos((uint32_t)(((uint64_t)(int64_t)where * turns[e]) >> 32), sn, cs);
+    cs_sm[i] = cs * p.factor;
+    cs_sm[D / 2 + i] = sn * p.factor;
+  }
+  __syncwarp();
   uint64_t c[INTER ? 8 : 4], s[INTER ? 8 : 4];
   if (rotates) {
-    if (!p.positions) pos[0] = pos[1] = pos[2] = at;
-    float cs[8], sn[8];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      const int i = 8 * u + e;
-      const int where = i < p.axis1 ? pos[0] : i < p.axis2 ? pos[1] : pos[2];
-      turn_sincos((uint32_t)(((uint64_t)(int64_t)where * (e & 1 ? turns[e >> 1].y : turns[e >> 1].x)) >> 32), sn[e], cs[e]);
-      sn[e] *= p.factor;
-      cs[e] *= p.factor;
-    }
-#pragma unroll
-    for (int e = 0; e < (INTER ? 8 : 4); ++e) {
-      c[e] = INTER ? f2_pack(cs[e], cs[e]) : f2_pack(cs[2 * e], cs[2 * e + 1]);
-      s[e] = INTER ? f2_pack(-sn[e], sn[e]) : f2_pack(sn[2 * e], sn[2 * e + 1]);
+    for (int e = 0; e < 2; ++e) {
+      const float4 cs = reinterpret_cast<const float4*>(cs_sm)[2 * u + e], sn = reinterpret_cast<const float4*>(cs_sm + D / 2)[2 * u + e];
+      if constexpr (INTER) {
+        c[4 * e] = f2_pack(cs.x, cs.x), c[4 * e + 1] = f2_pack(cs.y, cs.y), c[4 * e + 2] = f2_pack(cs.z, cs.z), c[4 * e + 3] = f2_pack(cs.w, cs.w);
+        s[4 * e] = f2_pack(-sn.x, sn.x), s[4 * e + 1] = f2_pack(-sn.y, sn.y), s[4 * e + 2] = f2_pack(-sn.z, sn.z), s[4 * e + 3] = f2_pack(-sn.w, sn.w);
+      } else {
+        c[2 * e] = f2_pack(cs.x, cs.y), c[2 * e + 1] = f2_pack(cs.z, cs.w);
+        s[2 * e] = f2_pack(sn.x, sn.y), s[2 * e + 1] = f2_pack(sn.z, sn.w);
+      }
     }
   }
   // queries
@@ -251,10 +260,11 @@ __device__ __forceinline__ void rope_rows(const RopeParams& p, uint32_t warp, in
 // ONE: the only CTA of the launch, which also counts the new tokens
 template <int D, bool INTER, bool ONE>
 __global__ void __launch_bounds__(ONE ? kRopeOneThreads : kRopeThreads, ONE ? 1 : kRopeCtas) rope_append_kernel(const __grid_constant__ RopeParams p, uint32_t n_warps) {
+  __shared__ __align__(16) float cs_sm[(ONE ? kRopeOneThreads : kRopeThreads) / 32][D];   // cosines and sines of a warp's token
   pdl_launch_next();
   pdl_wait();
   const uint32_t warp = blockIdx.x * (kRopeThreads / 32) + (threadIdx.x >> 5);
-  if (warp < n_warps) rope_rows<D, INTER>(p, warp, threadIdx.x & 31);
+  if (warp < n_warps) rope_rows<D, INTER>(p, cs_sm[threadIdx.x >> 5], warp, threadIdx.x & 31);
   if constexpr (ONE) {
     __syncthreads();                               // every thread has read the lengths
     for (int b = threadIdx.x; b < p.batch; b += blockDim.x) rope_count(p, b);
