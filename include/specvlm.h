@@ -9,6 +9,8 @@
  *   specvlm_draft_decode_attn   (gamma times) draft decode attention over the pruned cache
  *   specvlm_verify_attn     (gamma+1)-query causal verification attention over the full cache
  *   specvlm_accept          greedy acceptance length and next token
+ * Around it, for streams longer than what a model attends to: specvlm_rope_append_kv, specvlm_window_attn and the calls on a
+ * cache's pages (specvlm_reserve_pages, specvlm_release_pages, specvlm_fork_pages, specvlm_compact_pages).
  *
  * Conventions (all entry points)
  *   - Return value: SPECVLM_OK (0) or a negative specvlm_status code.  Argument errors are
