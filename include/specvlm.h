@@ -587,6 +587,14 @@ int32_t specvlm_debug_attn_give_up(const specvlm_kv_t* kv, const void* q, int32_
                                    int32_t* n_ctas, int32_t* d_status, void* stream);
 
 /*
+ * Test hook; the paper has no counterpart.  The same for specvlm_window_attn; n_ctas is 0 where the call runs on slices with the
+ * tensor cores (specvlm_debug_attn_merge has those), and nobody gives up then.
+ */
+int32_t specvlm_debug_window_give_up(const specvlm_kv_t* kv, const void* q, int32_t batch, int32_t n_q_heads, int32_t n_q,
+                                     int32_t window, int32_t n_sinks, float sm_scale, void* out, float* lse_or_null, void* ws,
+                                     size_t ws_bytes, int32_t lost_cta, int32_t* n_ctas, int32_t* d_status, void* stream);
+
+/*
  * Test hook, host only; the paper has no counterpart.  Reports how a verification window of n_q
  * query tokens at `group` = n_q_heads / n_kv_heads heads per KV head is cut into the parts that run
  * side by side in one launch: n_parts parts of q_per tokens (the last may be shorter), each of at

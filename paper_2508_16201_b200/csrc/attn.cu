@@ -836,7 +836,7 @@ static size_t rows16_ws_bytes(const specvlm_kv_t* kv, int32_t batch, int rows, b
 size_t attn_tc_ws_bytes(const specvlm_kv_t* kv, int32_t batch, int rows, int group);
 int32_t attn_tc_launch(const specvlm_kv_t* kv, const void* q, int32_t batch, int32_t n_q_heads, int32_t n_q,
                        float sm_scale, void* out, float* lse, void* ws, size_t ws_bytes, int32_t* d_status,
-                       cudaStream_t st, const int32_t* tree_parents, const KeyWindow* win = nullptr);
+                       cudaStream_t st, const int32_t* tree_parents, const KeyWindow* win = nullptr, int lost_cta = -1, int32_t* n_ctas = nullptr);
 
 template <int D, int STAGES, int NG, bool SPLIT, bool WIN>
 static int32_t launch_rows16_s(const CUtensorMap& tk, const CUtensorMap& tv, const AttnParams& p,
@@ -893,7 +893,7 @@ static int32_t attn_common(const specvlm_kv_t* kv, const void* q, int32_t batch,
   const int rows = group * n_q;
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   if (rows > kRows16Max)
-    return attn_tc_launch(kv, q, batch, n_q_heads, n_q, sm_scale, out, lse, ws, ws_bytes, d_status, st, nullptr, win);
+    return attn_tc_launch(kv, q, batch, n_q_heads, n_q, sm_scale, out, lse, ws, ws_bytes, d_status, st, nullptr, win, lost_cta, n_ctas);
 
   const int64_t lb64 = (int64_t)kv->n_layers * batch;
   if (lb64 > 65535 || kv->n_kv_heads > 65535) return SPECVLM_ERR_UNSUPPORTED_SHAPE;
@@ -1042,6 +1042,16 @@ extern "C" int32_t specvlm_window_attn(const specvlm_kv_t* kv, const void* q, in
   if (n_q > 9 || (int64_t)n_q_heads / kv->n_kv_heads * n_q > kWindowMaxRows) return SPECVLM_ERR_UNSUPPORTED_SHAPE;
   const KeyWindow win(kv, window, n_sinks);
   return attn_common(kv, q, batch, n_q_heads, n_q, sm_scale, out, lse_or_null, ws, ws_bytes, d_status, stream, -1, nullptr, &win);
+}
+
+extern "C" int32_t specvlm_debug_window_give_up(const specvlm_kv_t* kv, const void* q, int32_t batch, int32_t n_q_heads, int32_t n_q,
+                                                int32_t window, int32_t n_sinks, float sm_scale, void* out, float* lse_or_null,
+                                                void* ws, size_t ws_bytes, int32_t lost_cta, int32_t* n_ctas, int32_t* d_status,
+                                                void* stream) {
+  if (!kv || !n_ctas || window < 1 || n_sinks < 0 || n_q < 1 || kv->n_kv_heads < 1) return SPECVLM_ERR_INVALID_ARG;
+  if (n_q > 9 || (int64_t)n_q_heads / kv->n_kv_heads * n_q > kWindowMaxRows) return SPECVLM_ERR_UNSUPPORTED_SHAPE;
+  const KeyWindow win(kv, window, n_sinks);
+  return attn_common(kv, q, batch, n_q_heads, n_q, sm_scale, out, lse_or_null, ws, ws_bytes, d_status, stream, lost_cta, n_ctas, &win);
 }
 
 extern "C" size_t specvlm_verify_tree_workspace_bytes(const specvlm_kv_t* kv, int32_t batch, int32_t n_q_heads,

@@ -838,6 +838,10 @@ attn_tc_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__
       // A CTA's result counts where it has tiles; if a wait expired in any CTA the item is left alone.
       const int n_cta = p.n_cluster, rank = (int)blockIdx.x % n_cta;
       if (!active && st < rows) reinterpret_cast<float*>(big_ptr + C::OFF_Q)[st] = -INFINITY;      // a CTA without a tile
+      if (p.lost_cta == cta && st == 0) {                   // test hook: as if a wait of this CTA's had expired
+        *abort_flag = 1;
+        if (p.d_status) *p.d_status = SPECVLM_ERR_TIMEOUT;
+      }
       cluster_barrier();                                    // every role of every CTA has ended
       if (slice->first.item_tiles > 0) {
         const uint32_t part_o = smem_u32(big_ptr + C::OFF_K), part_lse = smem_u32(big_ptr + C::OFF_Q);
@@ -1194,7 +1198,7 @@ int32_t attn_pair_launch(const CUtensorMap& tk, const CUtensorMap& tv, const CUt
 
 int32_t attn_tc_launch(const specvlm_kv_t* kv, const void* q, int32_t batch, int32_t n_q_heads, int32_t n_q,
                        float sm_scale, void* out, float* lse, void* ws, size_t ws_bytes, int32_t* d_status,
-                       cudaStream_t st, const int32_t* tree_parents, const KeyWindow* win) {
+                       cudaStream_t st, const int32_t* tree_parents, const KeyWindow* win, int lost_cta, int32_t* n_ctas) {
   const int group = n_q_heads / kv->n_kv_heads;
   const int rows = group * n_q;
   if (group > 16 || batch > kSchedMaxBatch) return SPECVLM_ERR_UNSUPPORTED_SHAPE;
@@ -1223,6 +1227,8 @@ int32_t attn_tc_launch(const specvlm_kv_t* kv, const void* q, int32_t batch, int
     p.window = win->window;
     p.n_sinks = win->n_sinks;
     p.n_cluster = cluster;
+    p.lost_cta = lost_cta;
+    if (n_ctas) *n_ctas = cluster > 0 ? ctas : 0;           // (slices have a hook of their own: specvlm_debug_attn_merge)
     if (n_parts > 1) return SPECVLM_ERR_UNSUPPORTED_SHAPE;
   }
 

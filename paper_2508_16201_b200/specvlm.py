@@ -74,7 +74,7 @@ EXPORTS = [
     "specvlm_pages_workspace_bytes", "specvlm_reserve_pages", "specvlm_release_pages", "specvlm_fork_pages",
     "specvlm_compact_pages", "specvlm_debug_poison_shared_memory", "specvlm_debug_wait_timeout",
     "specvlm_debug_set_attn_splits", "specvlm_debug_window_parts", "specvlm_debug_attn_merge",
-    "specvlm_debug_attn_give_up",
+    "specvlm_debug_attn_give_up", "specvlm_debug_window_give_up",
 ]
 
 
@@ -148,6 +148,9 @@ def lib():
         L.specvlm_window_attn.restype = c_int32
         L.specvlm_window_attn.argtypes = [kvp, c_void_p, c_int32, c_int32, c_int32, c_int32, c_int32, c_float, c_void_p, c_void_p,
                                           c_void_p, c_size_t, c_void_p, c_void_p]
+        L.specvlm_debug_window_give_up.restype = c_int32
+        L.specvlm_debug_window_give_up.argtypes = [kvp, c_void_p, c_int32, c_int32, c_int32, c_int32, c_int32, c_float, c_void_p,
+                                                   c_void_p, c_void_p, c_size_t, c_int32, i32p, c_void_p, c_void_p]
         rowsp = POINTER(RowsStruct)
         L.specvlm_rope_turns.restype = c_int32
         L.specvlm_rope_turns.argtypes = [POINTER(ctypes.c_double), c_int32, POINTER(ctypes.c_uint64)]
@@ -722,6 +725,18 @@ def debug_attn_give_up(kv: KvCache, q: torch.Tensor, sm_scale: float, out: torch
     rc = lib().specvlm_debug_attn_give_up(byref(kv.struct), _ptr(q), B, Hq, float(sm_scale), _ptr(out), _ptr(lse), _ptr(ws),
                                           ws.numel(), int(lost_cta), byref(n), _ptr(d_status), _stream())
     _check(rc, "specvlm_debug_attn_give_up")
+    return n.value
+
+
+def debug_window_give_up(kv: KvCache, q: torch.Tensor, window: int, n_sinks: int, sm_scale: float, out: torch.Tensor,
+                         lse: torch.Tensor, ws: torch.Tensor, d_status: torch.Tensor, lost_cta: int = -1) -> int:
+    """window_attn with one CTA giving up as if a wait of its had expired; returns the number of CTAs, 0 on the tensor cores'
+    slices (test hook)."""
+    L, B, NQ, Hq, D = q.shape
+    n = c_int32()
+    rc = lib().specvlm_debug_window_give_up(byref(kv.struct), _ptr(q), B, Hq, NQ, window, n_sinks, float(sm_scale), _ptr(out),
+                                            _ptr(lse), _ptr(ws), ws.numel(), int(lost_cta), byref(n), _ptr(d_status), _stream())
+    _check(rc, "specvlm_debug_window_give_up")
     return n.value
 
 

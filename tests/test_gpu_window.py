@@ -221,6 +221,37 @@ def test_a_page_that_is_needed_and_not_mapped_is_reported():
                 assert int(st) == specvlm.ERR_INVALID_ARG and bool(torch.isfinite(out).all())
 
 
+@pytest.mark.parametrize("L,B,H,Hq,n_q,splits", [(1, 2, 2, 16, 6, 0), (1, 5, 4, 32, 6, 0), (1, 15, 4, 64, 4, 0), (1, 20, 5, 40, 6, 0),
+                                                 (1, 2, 2, 8, 1, 0), (1, 20, 4, 16, 1, 0), (1, 20, 4, 16, 1, 3), (4, 20, 4, 16, 1, 1)])
+def test_what_a_cta_that_gives_up_leaves(L, B, H, Hq, n_q, splits):
+    """Heads that the CTA has a part of keep what was there, the others are whole; the call says so, and the next is not
+    disturbed."""
+    W, S, D = 700, 70, 128
+    lens = [1000 - 90 * (b % 10) for b in range(B)]
+    cache, host = _cache(L, H, D, lens, n_q, W, S, page=64, seed=8)
+    q = synth.randn_bf16((L, B, n_q, Hq, D), "cuda", 8, "Q")
+    specvlm.debug_set_attn_splits(splits)
+    ws = torch.full((max(256, specvlm.window_attn_workspace_bytes(cache, B, Hq, n_q, W, S)),), 0xFF, dtype=torch.uint8, device="cuda")
+    want, want_lse = torch.empty_like(q), torch.empty(q.shape[:-1], dtype=torch.float32, device="cuda")
+    st = torch.zeros(1, dtype=torch.int32, device="cuda")
+    n = specvlm.debug_window_give_up(cache, q, W, S, 0.1, want, want_lse, ws, st)
+    assert n > 0 and int(st) == 0
+    _compare(want, want_lse, _reference(q, host, lens, W, S, 0.1))
+    for lost in sorted({0, 1, n // 2, n - 1}):
+        out, lse = torch.full_like(q, 7.0), torch.full_like(want_lse, 7.0)
+        st.zero_()
+        assert specvlm.debug_window_give_up(cache, q, W, S, 0.1, out, lse, ws, st, lost_cta=lost) == n
+        kept, left = lse == want_lse, lse == 7.0
+        assert bool((kept ^ left).all())
+        assert torch.equal(out[kept], want[kept]) and bool((out[left] == 7.0).all())
+        whole = left.view(L, B, n_q, H, Hq // H)
+        assert bool((whole == whole[:, :, :1, :, :1]).all())                        # a KV head's rows stand or fall together
+        # one item; on slices the items that the CTA has a part of, and none where it has no work
+        items = int(left.sum()) // (n_q * (Hq // H))
+        assert items == 1 if splits != 3 else items <= 2
+        assert int(st) == (specvlm.ERR_TIMEOUT if items else 0) and (items > 0 or lost == n - 1)
+
+
 def test_captured_calls_on_growing_sequences_and_one_workspace():
     """Two captured calls (decode and verification) share a workspace; lengths and tables change between the replays."""
     L, Hq, H, D, W, S = 2, 16, 2, 128, 200, 5
