@@ -799,14 +799,14 @@ attn_tc_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__
                 if (has1) acc += __uint_as_float(ob[k]) * w1[e];
                 res[2 * jj + x] = acc;
               }
-            if constexpr (CLUSTER) {
+            if (CLUSTER && p.n_cluster > 1) {
               // to this CTA's shared memory, where its K and V tiles were (every product of the item is complete)
               float* dst = reinterpret_cast<float*>(big_ptr + C::OFF_K) + r * kPartPitch + cc * 64 + lc;
 #pragma unroll
               for (int jj = 0; jj < 8; ++jj)
                 *reinterpret_cast<float2*>(dst + jj * 8) = make_float2(res[2 * jj], res[2 * jj + 1]);
               if ((lane & 3) == 0 && cc == 0) reinterpret_cast<float*>(big_ptr + C::OFF_Q)[r] = lse2[e];
-            } else if (complete) {
+            } else if (CLUSTER || complete) {
               const int t = r / p.group, hq = sg.g * p.group + (r - t * p.group);
               const size_t orow = ((size_t)lb * p.n_win + t) * p.n_q_heads + hq;
               __nv_bfloat16* dst = p.out + orow * D + cc * 64 + lc;
@@ -836,14 +836,15 @@ attn_tc_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__
 #undef SM_WAIT
     if constexpr (CLUSTER) {
       // A CTA's result counts where it has tiles; if a wait expired in any CTA the item is left alone.
+      // (A CTA alone has stored its rows already.)
       const int n_cta = p.n_cluster, rank = (int)blockIdx.x % n_cta;
       if (!active && st < rows) reinterpret_cast<float*>(big_ptr + C::OFF_Q)[st] = -INFINITY;      // a CTA without a tile
-      if (p.lost_cta == cta && st == 0) {                   // test hook: as if a wait of this CTA's had expired
+      if (n_cta > 1 && p.lost_cta == cta && st == 0) {      // test hook: as if a wait of this CTA's had expired
         *abort_flag = 1;
         if (p.d_status) *p.d_status = SPECVLM_ERR_TIMEOUT;
       }
-      cluster_barrier();                                    // every role of every CTA has ended
-      if (slice->first.item_tiles > 0) {
+      if (n_cta > 1) cluster_barrier();                     // every role of every CTA has ended
+      if (n_cta > 1 && slice->first.item_tiles > 0) {
         const uint32_t part_o = smem_u32(big_ptr + C::OFF_K), part_lse = smem_u32(big_ptr + C::OFF_Q);
         const int lb = slice->first.layer * p.batch + slice->first.b, g = slice->first.g;
         const uint32_t flag = smem_u32(const_cast<int*>(abort_flag));
@@ -890,11 +891,11 @@ attn_tc_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__
           if (p.lse && c4 == 0) p.lse[orow] = den > 0.f ? (mm + log2f(den)) * kLn2 : -INFINITY;
         }
       }
-      cluster_barrier_relaxed();                            // nobody reads this CTA's shared memory any more
+      if (n_cta > 1) cluster_barrier_relaxed();             // nobody reads this CTA's shared memory any more
     }
   }
   if constexpr (CLUSTER) {
-    if (warp < 4) {                                         // the other roles' part in the two barriers above
+    if (warp < 4 && p.n_cluster > 1) {                      // the other roles' part in the two barriers above
       cluster_barrier();
       cluster_barrier_relaxed();
     }
@@ -1122,7 +1123,7 @@ size_t attn_tc_ws_bytes(const specvlm_kv_t* kv, int32_t batch, int rows, int gro
 // (18 with more than 64 rows) around the bytes, with the merge kernel.  As many clusters as run side by side: 12 of eight CTAs do and 16 do not, 32 of
 // four and not 36, 72 of two.  Measured, 6 tokens of 8 heads per KV head at d = 128, cluster / slices: 8 items of 512 keys 8.6 /
 // 11.3 us, of 4096 12.7 / 14.9, of 16 384 24.6 / 22.7; 32 of 1024 12.5 / 18.8, of 4096 19.5 / 25.9; 64 of 4096 29.1 / 34.4; 96 of
-// 1024 19.8 / 24.6; 144 of 1024 22.7 / 22.5; 128 rows, 16 of 4096 21.4 / 25.5.  (The flags of the CTAs that gave up in the
+// 1024 17.1 / 24.6; 144 of 1024 20.0 / 22.5; 128 rows, 16 of 4096 21.4 / 25.5.  (The flags of the CTAs that gave up in the
 // LSEs, behind one more barrier of the CTA, instead of beside them: 0.4 us more with eight.)
 static int tc_cluster(const specvlm_kv_t* kv, int64_t items, int rows) {
   const int64_t tiles = (kv->max_seq_len + kBigTokens - 1) / kBigTokens;
@@ -1228,7 +1229,7 @@ int32_t attn_tc_launch(const specvlm_kv_t* kv, const void* q, int32_t batch, int
     p.n_sinks = win->n_sinks;
     p.n_cluster = cluster;
     p.lost_cta = lost_cta;
-    if (n_ctas) *n_ctas = cluster > 0 ? ctas : 0;           // (slices have a hook of their own: specvlm_debug_attn_merge)
+    if (n_ctas) *n_ctas = cluster > 1 ? ctas : 0;           // (slices have a hook of their own: specvlm_debug_attn_merge)
     if (n_parts > 1) return SPECVLM_ERR_UNSUPPORTED_SHAPE;
   }
 

@@ -221,7 +221,7 @@ def test_a_page_that_is_needed_and_not_mapped_is_reported():
                 assert int(st) == specvlm.ERR_INVALID_ARG and bool(torch.isfinite(out).all())
 
 
-@pytest.mark.parametrize("L,B,H,Hq,n_q,splits", [(1, 2, 2, 16, 6, 0), (1, 5, 4, 32, 6, 0), (1, 15, 4, 64, 4, 0), (1, 20, 5, 40, 6, 0),
+@pytest.mark.parametrize("L,B,H,Hq,n_q,splits", [(1, 2, 2, 16, 6, 0), (1, 5, 4, 32, 6, 0), (1, 15, 4, 64, 4, 0),
                                                  (1, 2, 2, 8, 1, 0), (1, 20, 4, 16, 1, 0), (1, 20, 4, 16, 1, 3), (4, 20, 4, 16, 1, 1)])
 def test_what_a_cta_that_gives_up_leaves(L, B, H, Hq, n_q, splits):
     """Heads that the CTA has a part of keep what was there, the others are whole; the call says so, and the next is not
