@@ -37,13 +37,17 @@ __device__ __forceinline__ void cluster_barrier() {
       "barrier.cluster.arrive.release.aligned;\n\t"
       "barrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
-// The same without the ordering of memory (and the wait for this thread's stores that it implies): what the threads
-// have read is read.
-__device__ __forceinline__ void cluster_barrier_relaxed() {
-  __syncwarp();
-  asm volatile(
-      "barrier.cluster.arrive.relaxed.aligned;\n\t"
-      "barrier.cluster.wait.aligned;" ::: "memory");
+// The end of a phase in which the CTAs read one another's shared memory.  Without the ordering of memory, and the wait for this
+// thread's stores that it implies (0.2 to 0.3 us), where the warp has used all that it has read (all_used), so that no read is
+// still on its way to a CTA that leaves.
+__device__ __forceinline__ void cluster_barrier_after_reads(bool all_used) {
+  if (__all_sync(0xffffffffu, all_used)) {
+    asm volatile(
+        "barrier.cluster.arrive.relaxed.aligned;\n\t"
+        "barrier.cluster.wait.aligned;" ::: "memory");
+  } else {
+    cluster_barrier();
+  }
 }
 // The address of this CTA's shared-memory word `addr` in the cluster's CTA `rank`
 __device__ __forceinline__ uint32_t cluster_map(uint32_t addr, int rank) {
