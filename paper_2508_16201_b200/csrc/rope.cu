@@ -43,6 +43,7 @@ struct RopeParams {
   int32_t n_rot;                                   // rotated channels / 16
   int32_t n_axes, axis1, axis2;                    // first pair of axis 1 and of axis 2
   int32_t counted, share;                          // share: warps that a token's rows are dealt out to
+  int32_t per_warp;                                // layers that a warp goes through
   float factor;
 };
 
@@ -121,7 +122,88 @@ __device__ __forceinline__ void turn_sincos(uint32_t turn, float& s, float& c) {
 constexpr int kRopeThreads = 128, kRopeOneThreads = 512, kRopeOneTokens = 8;
 constexpr int kRopeCtas = 8;                       // on an SM: 64 registers a thread
 constexpr int kRopeWarps = 48;                     // on an SM: with fewer tokens several warps share one
+constexpr int kRopeManyWarps = 128;                // on an SM, that are left where a warp takes several layers
+constexpr int kRopeLayerRounds = 4, kRopeLayerBatch = 2;
 constexpr int kRopeBatch = 2;         // rounds whose loads are in flight together
+
+// What a warp has to know of its token before it turns rows: loads that depend on nothing (ask), and what follows from them.
+template <int D, bool INTER>
+struct RopeToken {
+  static constexpr int kPerLane = D / 64;            // pairs of a lane: each angle is computed once a warp
+  int b, t, u;                                       // sequence, token, this thread's unit: 16 channels of a row
+  bool rotates;
+  int v0, dv;                                        // its vectors: v0, v0 + dv
+  int n_asked, len, pos[3];
+  uint64_t turns[kPerLane];
+  int blk, off;                                      // where the token's key and value go
+  bool stored;
+  uint64_t c[INTER ? 8 : 4], s[INTER ? 8 : 4];
+
+  __device__ __forceinline__ void ask(const RopeParams& p, int lane) {
+    constexpr int UNITS = D / 16;
+    u = lane % UNITS;
+    rotates = u < p.n_rot;
+    v0 = !INTER && rotates ? u : 2 * u;
+    dv = !INTER && rotates ? p.n_rot : 1;
+    n_asked = p.new_lens ? p.new_lens[b] : p.n_new;
+    len = p.seq_lens[b];
+    pos[0] = pos[1] = pos[2] = 0;
+    if (p.positions) {
+      const int32_t* const where = p.positions + (size_t)b * p.n_new + t;
+      const size_t axis = (size_t)p.batch * p.n_new;
+#pragma unroll
+      for (int a = 0; a < 3; ++a)
+        if (a < p.n_axes) pos[a] = where[a * axis];
+    }
+#pragma unroll
+    for (int e = 0; e < kPerLane; ++e) turns[e] = lane + 32 * e < 8 * p.n_rot ? p.turns[lane + 32 * e] : 0;
+  }
+
+  // false: the token's rows are padding, or its sequence is left alone
+  __device__ __forceinline__ bool find(const RopeParams& p, float* cs_sm, int lane) {
+    int start;
+    if (!rope_range(p, n_asked, len, start)) {
+      if (lane == 0 && p.d_status) *p.d_status = SPECVLM_ERR_INVALID_ARG;
+      return false;
+    }
+    if (t >= n_asked) return false;
+    const int at = start + t;
+    blk = b;
+    off = at;
+    stored = true;
+    if (p.table) {
+      const int nth = (int)((uint32_t)at / (uint32_t)p.block_tokens);
+      blk = p.table[(size_t)b * p.max_blocks + nth];
+      off = at - nth * p.block_tokens;
+      stored = blk >= 0 && blk < p.n_blocks;
+      if (!stored && lane == 0 && p.d_status) *p.d_status = SPECVLM_ERR_INVALID_ARG;
+    }
+    if (!p.positions) pos[0] = pos[1] = pos[2] = at;
+#pragma unroll
+    for (int e = 0; e < kPerLane; ++e) {
+      const int i = lane + 32 * e, where = i < p.axis1 ? pos[0] : i < p.axis2 ? pos[1] : pos[2];
+      float sn, cs;
+      turn_sincos((uint32_t)(((uint64_t)(int64_t)where * turns[e]) >> 32), sn, cs);
+      cs_sm[i] = cs * p.factor;
+      cs_sm[D / 2 + i] = sn * p.factor;
+    }
+    __syncwarp();
+    if (rotates) {
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        const float4 cs = reinterpret_cast<const float4*>(cs_sm)[2 * u + e], sn = reinterpret_cast<const float4*>(cs_sm + D / 2)[2 * u + e];
+        if constexpr (INTER) {
+          c[4 * e] = f2_pack(cs.x, cs.x), c[4 * e + 1] = f2_pack(cs.y, cs.y), c[4 * e + 2] = f2_pack(cs.z, cs.z), c[4 * e + 3] = f2_pack(cs.w, cs.w);
+          s[4 * e] = f2_pack(-sn.x, sn.x), s[4 * e + 1] = f2_pack(-sn.y, sn.y), s[4 * e + 2] = f2_pack(-sn.z, sn.z), s[4 * e + 3] = f2_pack(-sn.w, sn.w);
+        } else {
+          c[2 * e] = f2_pack(cs.x, cs.y), c[2 * e + 1] = f2_pack(cs.z, cs.w);
+          s[2 * e] = f2_pack(sn.x, sn.y), s[2 * e + 1] = f2_pack(sn.z, sn.w);
+        }
+      }
+    }
+    return true;
+  }
+};
 
 // A warp's rounds are the query rows first and then the key and value rows; those of a token are dealt out to `share` warps.
 template <int D, bool INTER>
@@ -130,26 +212,16 @@ __device__ __forceinline__ void rope_rows(const RopeParams& p, float* cs_sm, uin
   const uint32_t token = warp / (uint32_t)p.share, lb = token / (uint32_t)p.n_new;
   const int part = (int)(warp - token * p.share), t = (int)(token - lb * p.n_new);
   const int layer = (int)(lb / (uint32_t)p.batch), b = (int)(lb - (uint32_t)layer * p.batch);
-  const int u = lane % UNITS, sub = lane / UNITS, step = ROWS * p.share;
-  const bool rotates = u < p.n_rot;
-  const int v0 = !INTER && rotates ? u : 2 * u, dv = !INTER && rotates ? p.n_rot : 1;      // this thread's vectors: v0, v0 + dv
-  const uint4* q = p.q + layer * p.q_layer + b * p.q_batch + t * p.q_token + v0;
-
+  const int sub = lane / UNITS, step = ROWS * p.share;
   // All loads that depend on nothing are asked for together: the launch is one or two waves of short warps, whose time
   // is the number of round trips to memory one after the other.
-  const int n_asked = p.new_lens ? p.new_lens[b] : p.n_new, len = p.seq_lens[b];
-  int pos[3] = {0, 0, 0};
-  if (p.positions) {
-    const int32_t* const where = p.positions + (size_t)b * p.n_new + t;
-    const size_t axis = (size_t)p.batch * p.n_new;
-#pragma unroll
-    for (int a = 0; a < 3; ++a)
-      if (a < p.n_axes) pos[a] = where[a * axis];
-  }
-  constexpr int PER_LANE = D / 64;                  // pairs of a lane: each angle is computed once a warp
-  uint64_t turns[PER_LANE];
-#pragma unroll
-  for (int e = 0; e < PER_LANE; ++e) turns[e] = lane + 32 * e < 8 * p.n_rot ? p.turns[lane + 32 * e] : 0;
+  RopeToken<D, INTER> tok;
+  tok.b = b;
+  tok.t = t;
+  tok.ask(p, lane);
+  const bool rotates = tok.rotates;
+  const int v0 = tok.v0, dv = tok.dv;
+  const uint4* q = p.q + layer * p.q_layer + b * p.q_batch + t * p.q_token + v0;
   uint4 x[kRopeBatch], y[kRopeBatch];
   int row = part * ROWS + sub;
   const int64_t q_step = step * p.q_head;
@@ -162,47 +234,7 @@ __device__ __forceinline__ void rope_rows(const RopeParams& p, float* cs_sm, uin
     }
     src += q_step;
   }
-
-  int start;
-  if (!rope_range(p, n_asked, len, start)) {
-    if (lane == 0 && p.d_status) *p.d_status = SPECVLM_ERR_INVALID_ARG;
-    return;
-  }
-  if (t >= n_asked) return;
-  const int at = start + t;
-  int blk = b, off = at;
-  bool stored = true;
-  if (p.table) {
-    const int nth = (int)((uint32_t)at / (uint32_t)p.block_tokens);
-    blk = p.table[(size_t)b * p.max_blocks + nth];
-    off = at - nth * p.block_tokens;
-    stored = blk >= 0 && blk < p.n_blocks;
-    if (!stored && lane == 0 && p.d_status) *p.d_status = SPECVLM_ERR_INVALID_ARG;
-  }
-  if (!p.positions) pos[0] = pos[1] = pos[2] = at;
-#pragma unroll
-  for (int e = 0; e < PER_LANE; ++e) {
-    const int i = lane + 32 * e, where = i < p.axis1 ? pos[0] : i < p.axis2 ? pos[1] : pos[2];
-    float sn, cs;
-    turn_sincos((uint32_t)(((uint64_t)(int64_t)where * turns[e]) >> 32), sn, cs);
-    cs_sm[i] = cs * p.factor;
-    cs_sm[D / 2 + i] = sn * p.factor;
-  }
-  __syncwarp();
-  uint64_t c[INTER ? 8 : 4], s[INTER ? 8 : 4];
-  if (rotates) {
-#pragma unroll
-    for (int e = 0; e < 2; ++e) {
-      const float4 cs = reinterpret_cast<const float4*>(cs_sm)[2 * u + e], sn = reinterpret_cast<const float4*>(cs_sm + D / 2)[2 * u + e];
-      if constexpr (INTER) {
-        c[4 * e] = f2_pack(cs.x, cs.x), c[4 * e + 1] = f2_pack(cs.y, cs.y), c[4 * e + 2] = f2_pack(cs.z, cs.z), c[4 * e + 3] = f2_pack(cs.w, cs.w);
-        s[4 * e] = f2_pack(-sn.x, sn.x), s[4 * e + 1] = f2_pack(-sn.y, sn.y), s[4 * e + 2] = f2_pack(-sn.z, sn.z), s[4 * e + 3] = f2_pack(-sn.w, sn.w);
-      } else {
-        c[2 * e] = f2_pack(cs.x, cs.y), c[2 * e + 1] = f2_pack(cs.z, cs.w);
-        s[2 * e] = f2_pack(sn.x, sn.y), s[2 * e + 1] = f2_pack(sn.z, sn.w);
-      }
-    }
-  }
+  if (!tok.find(p, cs_sm, lane)) return;
   // queries
   const int64_t o_step = step * p.o_head;
   uint4* to = p.q_out + layer * p.o_layer + b * p.o_batch + t * p.o_token + row * p.o_head + v0;
@@ -210,7 +242,7 @@ __device__ __forceinline__ void rope_rows(const RopeParams& p, float* cs_sm, uin
 #pragma unroll
     for (int i = 0; i < kRopeBatch; ++i) {
       if (row + i * step < p.n_q_heads) {
-        if (rotates) turn_pairs<INTER>(x[i], y[i], c, s);
+        if (rotates) turn_pairs<INTER>(x[i], y[i], tok.c, tok.s);
         to[0] = x[i];
         to[dv] = y[i];
       }
@@ -227,11 +259,11 @@ __device__ __forceinline__ void rope_rows(const RopeParams& p, float* cs_sm, uin
     }
   }
   // keys and values, to the cache: their rounds go on where those of the queries end
-  if (!stored) return;
+  if (!tok.stored) return;
   const int q_rounds = (p.n_q_heads + ROWS - 1) / ROWS;
   int first = part - q_rounds % p.share;
   if (first < 0) first += p.share;
-  const int64_t dst = layer * p.s_layer + blk * p.s_block + off * p.s_token + v0;
+  const int64_t dst = layer * p.s_layer + tok.blk * p.s_block + tok.off * p.s_token + v0;
   const uint4* const nk = p.new_k + layer * p.k_layer + b * p.k_batch + t * p.k_token + v0;
   const uint4* const nv = p.new_v + layer * p.v_layer + b * p.v_batch + t * p.v_token + v0;
   for (row = first * ROWS + sub; row < 2 * p.n_kv_heads; row += kRopeBatch * step) {
@@ -248,7 +280,7 @@ __device__ __forceinline__ void rope_rows(const RopeParams& p, float* cs_sm, uin
     for (int i = 0; i < kRopeBatch; ++i) {
       const int h = row + i * step, g = h - p.n_kv_heads;
       if (g < p.n_kv_heads) {
-        if (rotates && g < 0) turn_pairs<INTER>(x[i], y[i], c, s);
+        if (rotates && g < 0) turn_pairs<INTER>(x[i], y[i], tok.c, tok.s);
         uint4* const into = g < 0 ? p.k + dst + h * p.s_head : p.v + dst + g * p.s_head;
         into[0] = x[i];
         into[dv] = y[i];
@@ -257,14 +289,75 @@ __device__ __forceinline__ void rope_rows(const RopeParams& p, float* cs_sm, uin
   }
 }
 
+// The same for many tokens of few heads: a warp takes p.per_warp layers of its token, whose lengths and angles are most of the
+// work then, and goes through the rows of all of them, eight or four at a time whichever layer they are of.
+template <int D, bool INTER>
+__device__ __forceinline__ void rope_layers(const RopeParams& p, float* cs_sm, uint32_t warp, int lane) {
+  constexpr int UNITS = D / 16, ROWS = 32 / UNITS;
+  const uint32_t lb = warp / (uint32_t)p.n_new;
+  const int t = (int)(warp - lb * p.n_new), nth = (int)(lb / (uint32_t)p.batch), b = (int)(lb - (uint32_t)nth * p.batch);
+  const int end = min((nth + 1) * p.per_warp, p.n_layers), n_rows = p.n_q_heads + 2 * p.n_kv_heads;
+  RopeToken<D, INTER> tok;
+  tok.b = b;
+  tok.t = t;
+  tok.ask(p, lane);
+  const int v0 = tok.v0, dv = tok.dv;
+  const uint4* const q = p.q + b * p.q_batch + t * p.q_token + v0;
+  const uint4* const nk = p.new_k + b * p.k_batch + t * p.k_token + v0;
+  const uint4* const nv = p.new_v + b * p.v_batch + t * p.v_token + v0;
+  if (!tok.find(p, cs_sm, lane)) return;
+  uint4* const o = p.q_out + b * p.o_batch + t * p.o_token + v0;
+  const int64_t dst = tok.blk * p.s_block + tok.off * p.s_token + v0;
+  int layer = nth * p.per_warp, row = lane / UNITS;
+  auto wrap = [&]() {
+    while (row >= n_rows) {
+      row -= n_rows;
+      ++layer;
+    }
+  };
+  wrap();
+  while (layer < end) {                             // (lanes of a warp may end a round apart)
+    uint4 x[kRopeLayerBatch], y[kRopeLayerBatch];
+    uint4* to[kRopeLayerBatch];
+    bool turn[kRopeLayerBatch];
+#pragma unroll
+    for (int i = 0; i < kRopeLayerBatch; ++i) {
+      to[i] = nullptr;
+      if (layer < end) {
+        const int h = row - p.n_q_heads, g = h - p.n_kv_heads;
+        const uint4* const src = h < 0 ? q + layer * p.q_layer + row * p.q_head : g < 0 ? nk + layer * p.k_layer + h * p.k_head
+                                                                                          : nv + layer * p.v_layer + g * p.v_head;
+        x[i] = src[0];
+        y[i] = src[dv];
+        turn[i] = g < 0 && tok.rotates;
+        if (h < 0) to[i] = o + layer * p.o_layer + row * p.o_head;
+        else if (tok.stored) to[i] = (g < 0 ? p.k + h * p.s_head : p.v + g * p.s_head) + (dst + layer * p.s_layer);
+      }
+      row += ROWS;
+      wrap();
+    }
+#pragma unroll
+    for (int i = 0; i < kRopeLayerBatch; ++i) {
+      if (to[i]) {
+        if (turn[i]) turn_pairs<INTER>(x[i], y[i], tok.c, tok.s);
+        to[i][0] = x[i];
+        to[i][dv] = y[i];
+      }
+    }
+  }
+}
+
 // ONE: the only CTA of the launch, which also counts the new tokens
-template <int D, bool INTER, bool ONE>
+template <int D, bool INTER, bool ONE, bool LAYERS = false>
 __global__ void __launch_bounds__(ONE ? kRopeOneThreads : kRopeThreads, ONE ? 1 : kRopeCtas) rope_append_kernel(const __grid_constant__ RopeParams p, uint32_t n_warps) {
   __shared__ __align__(16) float cs_sm[(ONE ? kRopeOneThreads : kRopeThreads) / 32][D];   // cosines and sines of a warp's token
   pdl_launch_next();
   pdl_wait();
   const uint32_t warp = blockIdx.x * (kRopeThreads / 32) + (threadIdx.x >> 5);
-  if (warp < n_warps) rope_rows<D, INTER>(p, cs_sm[threadIdx.x >> 5], warp, threadIdx.x & 31);
+  if (warp < n_warps) {
+    if constexpr (LAYERS) rope_layers<D, INTER>(p, cs_sm[threadIdx.x >> 5], warp, threadIdx.x & 31);
+    else rope_rows<D, INTER>(p, cs_sm[threadIdx.x >> 5], warp, threadIdx.x & 31);
+  }
   if constexpr (ONE) {
     __syncthreads();                               // every thread has read the lengths
     for (int b = threadIdx.x; b < p.batch; b += blockDim.x) rope_count(p, b);
@@ -287,7 +380,8 @@ static int32_t launch_rope(const RopeParams& p, uint32_t n_warps, cudaStream_t s
   if (!p.counted && n_warps <= kRopeOneThreads / 32)
     return launch_after(rope_append_kernel<D, INTER, true>, dim3(1), dim3(32 * n_warps), 0, st, p, n_warps);
   const uint32_t blocks = (n_warps + kRopeThreads / 32 - 1) / (kRopeThreads / 32);
-  const int32_t rc = launch_after(rope_append_kernel<D, INTER, false>, dim3(blocks), dim3(kRopeThreads), 0, st, p, n_warps);
+  const int32_t rc = launch_after(p.per_warp > 1 ? rope_append_kernel<D, INTER, false, true> : rope_append_kernel<D, INTER, false>,
+                                  dim3(blocks), dim3(kRopeThreads), 0, st, p, n_warps);
   if (rc != SPECVLM_OK || p.counted) return rc;
   return launch_after(rope_count_kernel, dim3((unsigned)((p.batch + 127) / 128)), dim3(128), 0, st, p);
 }
@@ -401,7 +495,11 @@ extern "C" int32_t specvlm_rope_append_kv(const specvlm_kv_t* kv, const specvlm_
   p.share = (int32_t)(share < rounds ? share : rounds);
   // few tokens that have to be counted: one CTA, which spares the second launch
   if (!counted && tokens <= kRopeOneTokens && p.share > kRopeOneThreads / 32 / tokens) p.share = (int32_t)(kRopeOneThreads / 32 / tokens);
-  const uint32_t n_warps = (uint32_t)(tokens * p.share);   // < 2^31: more than a warp a token only for few tokens
+  // many tokens of few rows: a warp takes as many layers as leave four times the warps that the SMs hold
+  const int64_t layers = rounds <= kRopeLayerRounds ? tokens / ((int64_t)sm_count() * kRopeManyWarps) : 1;
+  p.per_warp = (int32_t)(layers < 2 ? 1 : layers < c.n_layers ? layers : c.n_layers);
+  const uint32_t n_warps = p.per_warp > 1 ? (uint32_t)((c.n_layers + p.per_warp - 1) / p.per_warp * ((int64_t)batch * n_new))
+                                          : (uint32_t)(tokens * p.share);   // < 2^31: more than a warp a token only for few tokens
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   if (c.head_dim == 128)
     return rope->interleaved ? launch_rope<128, true>(p, n_warps, st) : launch_rope<128, false>(p, n_warps, st);
