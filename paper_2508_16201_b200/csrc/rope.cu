@@ -43,7 +43,7 @@ struct RopeParams {
   int32_t n_rot;                                   // rotated channels / 16
   int32_t n_axes, axis1, axis2;                    // first pair of axis 1 and of axis 2
   int32_t counted, share;                          // share: warps that a token's rows are dealt out to
-  int32_t per_warp;                                // layers that a warp goes through
+  int32_t per_warp;                                // layers that a warp goes through (rope_layers), 0: rope_rows
   float factor;
 };
 
@@ -380,7 +380,7 @@ static int32_t launch_rope(const RopeParams& p, uint32_t n_warps, cudaStream_t s
   if (!p.counted && n_warps <= kRopeOneThreads / 32)
     return launch_after(rope_append_kernel<D, INTER, true>, dim3(1), dim3(32 * n_warps), 0, st, p, n_warps);
   const uint32_t blocks = (n_warps + kRopeThreads / 32 - 1) / (kRopeThreads / 32);
-  const int32_t rc = launch_after(p.per_warp > 1 ? rope_append_kernel<D, INTER, false, true> : rope_append_kernel<D, INTER, false>,
+  const int32_t rc = launch_after(p.per_warp > 0 ? rope_append_kernel<D, INTER, false, true> : rope_append_kernel<D, INTER, false>,
                                   dim3(blocks), dim3(kRopeThreads), 0, st, p, n_warps);
   if (rc != SPECVLM_OK || p.counted) return rc;
   return launch_after(rope_count_kernel, dim3((unsigned)((p.batch + 127) / 128)), dim3(128), 0, st, p);
@@ -495,10 +495,12 @@ extern "C" int32_t specvlm_rope_append_kv(const specvlm_kv_t* kv, const specvlm_
   p.share = (int32_t)(share < rounds ? share : rounds);
   // few tokens that have to be counted: one CTA, which spares the second launch
   if (!counted && tokens <= kRopeOneTokens && p.share > kRopeOneThreads / 32 / tokens) p.share = (int32_t)(kRopeOneThreads / 32 / tokens);
-  // many tokens of few rows: a warp takes as many layers as leave four times the warps that the SMs hold
-  const int64_t layers = rounds <= kRopeLayerRounds ? tokens / ((int64_t)sm_count() * kRopeManyWarps) : 1;
-  p.per_warp = (int32_t)(layers < 2 ? 1 : layers < c.n_layers ? layers : c.n_layers);
-  const uint32_t n_warps = p.per_warp > 1 ? (uint32_t)((c.n_layers + p.per_warp - 1) / p.per_warp * ((int64_t)batch * n_new))
+  // Many tokens of few rows: a warp takes as many layers as leave four times the warps that the SMs hold (rope_layers; with one
+  // layer a warp it still gains, as key and value rows share the queries' rounds).  8 + 2 heads of d = 64, 25 layers of 8723
+  // tokens 168 -> 135 us, one of 32 000 27.5 -> 25.6; 4 + 1 heads 28 layers of 8000 163 -> 70, one of 32 000 25.8 -> 21.3.
+  const int64_t layers = rounds <= kRopeLayerRounds ? tokens / ((int64_t)sm_count() * kRopeManyWarps) : 0;
+  p.per_warp = (int32_t)(layers < c.n_layers ? layers : c.n_layers);
+  const uint32_t n_warps = p.per_warp > 0 ? (uint32_t)((c.n_layers + p.per_warp - 1) / p.per_warp * ((int64_t)batch * n_new))
                                           : (uint32_t)(tokens * p.share);   // < 2^31: more than a warp a token only for few tokens
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   if (c.head_dim == 128)

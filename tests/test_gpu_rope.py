@@ -165,6 +165,43 @@ def test_layer_by_layer_equals_all_layers():
         assert torch.equal(torch.nan_to_num(a, 9.0), torch.nan_to_num(b, 9.0))
 
 
+@pytest.mark.parametrize("Hq,H,D,inter,rot", [(4, 1, 64, False, 64), (8, 2, 64, True, 48), (5, 1, 128, False, 32), (0, 3, 64, False, 16)])
+@pytest.mark.parametrize("L,B,n", [(7, 2, 3000), (23, 3, 900), (1, 5, 4000)])
+def test_many_tokens_of_few_heads(Hq, H, D, inter, rot, L, B, n):
+    """Enough tokens for warps that take several layers of one, a number that does not divide the layers among them: the same
+    bits as layer by layer, whose calls are smaller; ragged, with a page that is not mapped, and padding left alone."""
+    news = [n - 37 * b for b in range(B)]
+    starts = [0] + [61 + b for b in range(1, B)]
+    caps = [s + n for s in starts]
+    freq = torch.from_numpy(rolling.frequencies(rot, 1e4))
+    rope = specvlm.Rope(freq, interleaved=inter, factor=1.1)
+    results = []
+    for whole in (True, False):
+        cache, rows = _problem(L, B, n, max(Hq, 1), H, D, starts, caps, page=64, seed=13)
+        cache.block_table[B - 1, 2] = -1
+        q = rows[0] if Hq else None
+        out = torch.full(rows[0].shape, 7.0, dtype=torch.bfloat16, device="cuda") if Hq else None
+        new_lens = torch.tensor(news, dtype=torch.int32, device="cuda")
+        st = torch.zeros(1, dtype=torch.int32, device="cuda")
+        if whole:
+            specvlm.rope_append_kv(cache, rope, q, rows[1], rows[2], q_out=out, new_lens=new_lens, d_status=st)
+        else:
+            for layer in range(L):
+                for b in range(B):                               # one sequence at a time: few tokens a call
+                    one = specvlm.KvCache(cache.k[layer:layer + 1], cache.v[layer:layer + 1], cache.seq_lens[b:b + 1].clone(),
+                                          cache.max_seq_len, cache.block_table[b:b + 1])
+                    cut = [x[layer:layer + 1, b:b + 1] if x is not None else None for x in (q, rows[1], rows[2], out)]
+                    specvlm.rope_append_kv(one, rope, *cut[:3], q_out=cut[3], new_lens=new_lens[b:b + 1], d_status=st)
+            cache.seq_lens += new_lens
+        assert int(st) == specvlm.ERR_INVALID_ARG and cache.seq_lens.tolist() == [s + m for s, m in zip(starts, news)]
+        results.append((torch.nan_to_num(cache.k, 9.0), torch.nan_to_num(cache.v, 9.0), out))
+    for a, b in zip(*results):
+        assert a is None or torch.equal(a, b)
+    if Hq:
+        for b, m in enumerate(news):
+            assert bool((results[0][2][:, b, m:] == 7.0).all()) and not bool((results[0][2][:, b, :m] == 7.0).all(-1).any())
+
+
 @pytest.mark.parametrize("counted", [False, True])
 @pytest.mark.parametrize("n", [2, 60])
 def test_sequences_out_of_range_are_left_alone(counted, n):
