@@ -587,7 +587,8 @@ int32_t specvlm_debug_attn_give_up(const specvlm_kv_t* kv, const void* q, int32_
                                    int32_t* n_ctas, int32_t* d_status, void* stream);
 
 /*
- * Test hook; the paper has no counterpart.  The same for specvlm_window_attn; n_ctas is 0 where the call runs on the tensor cores
+ * Test hook; the paper has no counterpart.  The same for specvlm_window_attn, where what stays as it is are the rows (query
+ * tokens and heads of a KV head) that the CTA has a part of, all of a KV head or 16 of them; n_ctas is 0 where the call runs on the tensor cores
  * without clusters of two or more CTAs, and nobody gives up then.
  */
 int32_t specvlm_debug_window_give_up(const specvlm_kv_t* kv, const void* q, int32_t batch, int32_t n_q_heads, int32_t n_q,

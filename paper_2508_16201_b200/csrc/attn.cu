@@ -24,10 +24,10 @@ struct Rows16 {
   float m0, m1, l0, l1;
   int lim0, lim1;                                 // visible keys of the two rows this thread holds
 
-  // P: AttnParams or AttnTcParams (n_q: query tokens of the window, lb: layer * batch + sequence)
+  // P: AttnParams or AttnTcParams (n_q: query tokens of the window, lb: layer * batch + sequence; the rows base .. rows - 1)
   template <typename P>
-  __device__ __forceinline__ void start(const P& p, int n_q, int rows, size_t lb, int g, int kv_len, int lane) {
-    const int row0 = lane >> 2, row1 = row0 + 8, col = (lane & 3) * 2;
+  __device__ __forceinline__ void start(const P& p, int n_q, int rows, size_t lb, int g, int kv_len, int lane, int base = 0) {
+    const int row0 = base + (lane >> 2), row1 = row0 + 8, col = (lane & 3) * 2;
     const __nv_bfloat16* q0 = nullptr;
     const __nv_bfloat16* q1 = nullptr;
     lim0 = lim1 = 0;
@@ -271,7 +271,10 @@ __device__ __forceinline__ void rows16_consume(const AttnParams& p, uint8_t* sme
   constexpr int OPITCH = Rows16<D>::OPITCH;
   const uint32_t bar_full = base + STAGES * STAGE_BYTES, bar_empty = bar_full + 8 * STAGES;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-  const int g = blockIdx.y, lb = blockIdx.z;
+  const int g = WIN ? (int)blockIdx.y / p.row_groups : (int)blockIdx.y, lb = blockIdx.z;
+  // this item's rows: all, or a group of 16
+  const int base_row = WIN ? 16 * ((int)blockIdx.y - g * p.row_groups) : 0;
+  const int rows = WIN && p.rows - base_row > 16 ? 16 : p.rows - base_row;
   const bool spec = !WIN && p.block_table == nullptr;
   const int kv_len = view.len;
   const int n_all = (kv_len + kTileTokens - 1) / kTileTokens;
@@ -279,8 +282,8 @@ __device__ __forceinline__ void rows16_consume(const AttnParams& p, uint8_t* sme
   if (n_all == 0) {
     // An empty sequence: its outputs are zero, its LSE -inf.  The ring stays untouched: the tile that the producer
     // asked for before it knew the length may still be landing there, with whatever the cache rows hold.
-    for (int idx = tid; idx < p.rows * (D / 8); idx += 128 * NG) {
-      const int r = idx / (D / 8), c8 = idx - r * (D / 8);
+    for (int idx = tid; idx < rows * (D / 8); idx += 128 * NG) {
+      const int r = base_row + idx / (D / 8), c8 = idx % (D / 8);
       const int t = r / p.group, h = g * p.group + (r - t * p.group);
       const size_t orow = ((size_t)lb * p.n_q + t) * p.n_q_heads + h;
       *reinterpret_cast<uint4*>(p.out + orow * D + c8 * 8) = make_uint4(0, 0, 0, 0);
@@ -291,7 +294,7 @@ __device__ __forceinline__ void rows16_consume(const AttnParams& p, uint8_t* sme
   const int cw = warp & 3, grp = warp >> 2;                           // token slice, consumer group
   Rows16<D> st;
   // (positions of the newest keys are as far apart as the keys)
-  st.start(p, p.n_q, p.rows, lb, g, kv_len, lane);
+  st.start(p, p.n_q, base_row + rows, lb, g, kv_len, lane, base_row);
   bool alive = true;
   // a CTA without a tile of its own: the one asked for before the length was known lands where the merge buffer will be
   if (SPLIT && n_my == 0 && spec && !mbar_wait(bar_full, 0, abort_flag)) alive = false;
@@ -324,14 +327,14 @@ __device__ __forceinline__ void rows16_consume(const AttnParams& p, uint8_t* sme
   float* const o_sm = reinterpret_cast<float*>(smem);                  // [NW][16][OPITCH]
   float* const m_sm = o_sm + NW * 16 * OPITCH;                         // [NW][16]
   float* const l_sm = m_sm + NW * 16;                                  // [NW][16]
-  st.publish(o_sm, m_sm, l_sm, p.rows, warp, lane);
+  st.publish(o_sm, m_sm, l_sm, rows, warp, lane);
   asm volatile("bar.sync 1, %0;" ::"n"(128 * NG) : "memory");
   if constexpr (SPLIT) {
     // This CTA's result, normalised, behind the merge buffer, and its log-sum-exps, for the whole cluster to read.  The
     // latter say whether the CTA gave up, and lie behind the ring, where no copy that was asked for before lands on them.
     float* const part_o = l_sm + NW * 16;                              // [16][D]
     float* const part_lse = reinterpret_cast<float*>(smem + STAGES * STAGE_BYTES + 16 * STAGES + 16);   // [16]
-    for (int idx = tid; idx < p.rows * (D / 4); idx += 128 * NG) {
+    for (int idx = tid; idx < rows * (D / 4); idx += 128 * NG) {
       const int r = idx / (D / 4), c = (idx - r * (D / 4)) * 4;
       float4 acc;
       const float lse2 = rows16_merge<D, NW>(o_sm, m_sm, l_sm, r, c, acc);
@@ -340,7 +343,7 @@ __device__ __forceinline__ void rows16_consume(const AttnParams& p, uint8_t* sme
     }
     cluster_barrier();
     bool all_used = true;
-    for (int idx = rank * 128 * NG + tid; idx < p.rows * (D / 4); idx += n_cta * 128 * NG) {
+    for (int idx = rank * 128 * NG + tid; idx < rows * (D / 4); idx += n_cta * 128 * NG) {
       const int r = idx / (D / 4), c = (idx - r * (D / 4)) * 4;
       float lse[kMaxRows16Cluster];
       float4 x[kMaxRows16Cluster];
@@ -375,7 +378,7 @@ __device__ __forceinline__ void rows16_consume(const AttnParams& p, uint8_t* sme
         den += w;
       }
       const float inv = den > 0.f ? 1.f / den : 0.f;
-      const int t = r / p.group, h = g * p.group + (r - t * p.group);
+      const int t = (base_row + r) / p.group, h = g * p.group + (base_row + r - t * p.group);
       const size_t orow = ((size_t)lb * p.n_q + t) * p.n_q_heads + h;
       store_bf16x4(p.out + orow * D + c, make_float4(acc.x * inv, acc.y * inv, acc.z * inv, acc.w * inv));
       if (p.lse && c == 0) p.lse[orow] = den > 0.f ? (mm + log2f(den)) * kLn2 : -INFINITY;
@@ -384,11 +387,11 @@ __device__ __forceinline__ void rows16_consume(const AttnParams& p, uint8_t* sme
     if (gave_up && tid == 0) await_copies<STAGES>(bar_full, abort_flag);
     return;
   }
-  for (int idx = tid; idx < p.rows * (D / 4); idx += 128 * NG) {
+  for (int idx = tid; idx < rows * (D / 4); idx += 128 * NG) {
     const int r = idx / (D / 4), c = (idx - r * (D / 4)) * 4;
     float4 acc;
     const float lse2 = rows16_merge<D, NW>(o_sm, m_sm, l_sm, r, c, acc);
-    const int t = r / p.group, h = g * p.group + (r - t * p.group);
+    const int t = (base_row + r) / p.group, h = g * p.group + (base_row + r - t * p.group);
     const size_t orow = ((size_t)lb * p.n_q + t) * p.n_q_heads + h;
     store_bf16x4(p.out + orow * D + c, acc);
     if (p.lse && c == 0) p.lse[orow] = lse2 * kLn2;
@@ -427,7 +430,7 @@ attn_rows16_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_consta
   volatile int* const abort_flag = reinterpret_cast<volatile int*>(smem + STAGES * STAGE_BYTES + 16 * STAGES);
 
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-  const int g = blockIdx.y, lb = blockIdx.z;
+  const int g = WIN ? (int)blockIdx.y / p.row_groups : (int)blockIdx.y, lb = blockIdx.z;
   const int layer = lb / p.batch, b = lb - layer * p.batch;
   const int rank = SPLIT ? (int)blockIdx.x : 0, n_cta = SPLIT ? (int)gridDim.x : 1;
 
@@ -838,6 +841,7 @@ static size_t rows16_ws_bytes(const specvlm_kv_t* kv, int32_t batch, int rows, b
 
 // tcgen05 path (attn_tc.cu)
 size_t attn_tc_ws_bytes(const specvlm_kv_t* kv, int32_t batch, int rows, int group);
+double attn_tc_window_us(const specvlm_kv_t* kv, int32_t batch, int rows);      // estimate for a call with a window
 int32_t attn_tc_launch(const specvlm_kv_t* kv, const void* q, int32_t batch, int32_t n_q_heads, int32_t n_q,
                        float sm_scale, void* out, float* lse, void* ws, size_t ws_bytes, int32_t* d_status,
                        cudaStream_t st, const int32_t* tree_parents, const KeyWindow* win = nullptr, int lost_cta = -1, int32_t* n_ctas = nullptr);
@@ -883,6 +887,34 @@ __global__ void give_up_kernel(const __grid_constant__ AttnTcParams p, int gcta,
   unwritten_parts(p, gcta, head_dim, threadIdx.x, blockDim.x);
 }
 
+// Groups of 16 rows that a call with a window and more than 16 rows is cut into for the kernels above, each with CTAs of its own
+// that read the same tiles (all but the first from the L2 cache); 1: none, the tcgen05 kernel.  For short windows and few items the
+// time is what is around the tiles, and that is 4 us here against 8 to 12 there.  Estimated us: 3.9 around the tiles of an item
+// that has an SM, one more for a cluster; beyond, rounds of two CTAs an SM (d = 64: four) with 4.4 around their tiles of 0.75
+// (0.98) each.  Measured, groups / tcgen05, d = 128, 48 rows: 8 items of 64 / 512 / 2048 / 4096 keys 5.1 / 6.3 / 9.2 / 13.3 against
+// 8.7 / 8.6 / 10.6 / 12.9; 32 of 64 / 512 / 1024 5.3 / 8.2 / 11.8 against 9.2 / 10.5 / 12.8; 96 of 64 / 512 6.4 / 11.3 against 9.3 /
+// 12.8; 624 (42 rows) of 55 / 256 37.4 / 50.5 against 35.6 / 46.1, with 21 rows 256 / 1024 35.9 / 77.9 against 44.2 / 68.3; d = 64, 32
+// rows, 448 of 64 / 512 / 1024 11.2 / 21.5 / 33.5 against 24.3 / 31.5 / 38.9.
+static int window_row_groups(const specvlm_kv_t* kv, int32_t batch, int rows) {
+  const int groups = (rows + kRows16Max - 1) / kRows16Max;
+  const int64_t items = (int64_t)kv->n_layers * batch * kv->n_kv_heads, n_groups = items * groups, sms = sm_count();
+  const int64_t tiles = (kv->max_seq_len + kTileTokens - 1) / kTileTokens;
+  if ((int64_t)kv->n_layers * batch > 65535 || (int64_t)kv->n_kv_heads * groups > 65535) return 1;
+  const double hbm_us = (double)items * kv->max_seq_len * (4.0 * kv->head_dim) / 6.5e6;
+  double us;
+  if (n_groups <= sms) {
+    const int n = rows16_cluster(kv, n_groups, tiles, true);
+    us = 3.9 + (n > 1 ? 1.0 : 0.0) + 1.08 * rows16_tile_us(kv) * (double)((tiles + n - 1) / n);
+  } else if (kv->head_dim == 64 && n_groups <= 2 * sms) {
+    us = 4.2 + 0.5 * (double)tiles;
+  } else {
+    const double rounds = (double)n_groups / (kv->head_dim == 64 ? 4 * sms : 2 * sms);
+    us = (rounds > 1.0 ? rounds : 1.0) * (4.4 + (kv->head_dim == 64 ? 0.98 : 0.75) * (double)tiles);
+  }
+  if (us < 3.9 + hbm_us) us = 3.9 + hbm_us;
+  return us < attn_tc_window_us(kv, batch, rows) ? groups : 1;
+}
+
 static int32_t attn_common(const specvlm_kv_t* kv, const void* q, int32_t batch, int32_t n_q_heads,
                            int32_t n_q, float sm_scale, void* out, float* lse, void* ws,
                            size_t ws_bytes, int32_t* d_status, void* stream, int lost_cta = -1, int32_t* n_ctas = nullptr,
@@ -896,20 +928,26 @@ static int32_t attn_common(const specvlm_kv_t* kv, const void* q, int32_t batch,
   if (group > 16 || n_q > 9) return SPECVLM_ERR_UNSUPPORTED_SHAPE;
   const int rows = group * n_q;
   cudaStream_t st = static_cast<cudaStream_t>(stream);
-  if (rows > kRows16Max)
+  const specvlm_kv_t sched = win ? win->view(kv, n_q) : *kv;
+  if (win && rows > kRows16Max) {          // what the tcgen05 kernel asks for, whichever is chosen
+    if (batch > kSchedMaxBatch) return SPECVLM_ERR_UNSUPPORTED_SHAPE;
+    if (!ws || (reinterpret_cast<uintptr_t>(ws) & 255u)) return SPECVLM_ERR_INVALID_ARG;
+    if (ws_bytes < attn_tc_ws_bytes(&sched, batch, rows, group)) return SPECVLM_ERR_WORKSPACE_TOO_SMALL;
+  }
+  const int row_groups = win && rows > kRows16Max ? window_row_groups(&sched, batch, rows) : 1;
+  if (rows > kRows16Max && row_groups == 1)
     return attn_tc_launch(kv, q, batch, n_q_heads, n_q, sm_scale, out, lse, ws, ws_bytes, d_status, st, nullptr, win, lost_cta, n_ctas);
 
   const int64_t lb64 = (int64_t)kv->n_layers * batch;
-  if (lb64 > 65535 || kv->n_kv_heads > 65535) return SPECVLM_ERR_UNSUPPORTED_SHAPE;
+  if (lb64 > 65535 || kv->n_kv_heads * row_groups > 65535) return SPECVLM_ERR_UNSUPPORTED_SHAPE;
   CUtensorMap tk, tv;
   rc = encode_kv_map(&tk, kv, kv->k, kTileTokens);
   if (rc != SPECVLM_OK) return rc;
   rc = encode_kv_map(&tv, kv, kv->v, kTileTokens);
   if (rc != SPECVLM_OK) return rc;
 
-  const specvlm_kv_t sched = win ? win->view(kv, n_q) : *kv;
-  int scratch_ctas;
-  const int ctas = rows16_slices(&sched, batch, &scratch_ctas, win != nullptr);
+  int scratch_ctas = 0;
+  const int ctas = row_groups > 1 ? 0 : rows16_slices(&sched, batch, &scratch_ctas, win != nullptr);
   if (scratch_ctas > 0) {
     if (!ws || (reinterpret_cast<uintptr_t>(ws) & 255u)) return SPECVLM_ERR_INVALID_ARG;
     if (ws_bytes < rows16_scratch_bytes(kv, scratch_ctas, rows)) return SPECVLM_ERR_WORKSPACE_TOO_SMALL;
@@ -950,9 +988,10 @@ static int32_t attn_common(const specvlm_kv_t* kv, const void* q, int32_t batch,
   p.window = win ? win->window : 0;
   p.n_sinks = win ? win->n_sinks : 0;
   p.n_blocks = kv->n_blocks;
+  p.row_groups = row_groups;
 
-  const int n = rows16_cluster(&sched, lb64 * kv->n_kv_heads, (sched.max_seq_len + kTileTokens - 1) / kTileTokens, win != nullptr);
-  dim3 grid((unsigned)n, (unsigned)kv->n_kv_heads, (unsigned)lb64);
+  const int n = rows16_cluster(&sched, lb64 * kv->n_kv_heads * row_groups, (sched.max_seq_len + kTileTokens - 1) / kTileTokens, win != nullptr);
+  dim3 grid((unsigned)n, (unsigned)(kv->n_kv_heads * row_groups), (unsigned)lb64);
   if (n_ctas) *n_ctas = (int32_t)(grid.x * grid.y * grid.z);
   if (win) return kv->head_dim == 128 ? launch_rows16<128, true>(tk, tv, p, grid, st) : launch_rows16<64, true>(tk, tv, p, grid, st);
   return kv->head_dim == 128 ? launch_rows16<128, false>(tk, tv, p, grid, st) : launch_rows16<64, false>(tk, tv, p, grid, st);

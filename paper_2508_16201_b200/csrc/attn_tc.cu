@@ -1123,27 +1123,39 @@ size_t attn_tc_ws_bytes(const specvlm_kv_t* kv, int32_t batch, int rows, int gro
 }
 
 // CTAs per item of a call with a window, whose items are all about as long: a cluster each (of one CTA, too), or 0 for slices and
-// their merge.  A cluster costs 7.8 us around its CTAs' tiles, which take 0.7 to 1.3 us each, or around the bytes; slices 12.3
-// (18 with more than 64 rows) around the bytes, with the merge kernel.  As many clusters as run side by side: 12 of eight CTAs do and 16 do not, 32 of
-// four and not 36, 72 of two.  Measured, 6 tokens of 8 heads per KV head at d = 128, cluster / slices: 8 items of 512 keys 8.6 /
-// 11.3 us, of 4096 12.7 / 14.9, of 16 384 24.6 / 22.7; 32 of 1024 12.5 / 18.8, of 4096 19.5 / 25.9; 64 of 4096 29.1 / 34.4; 96 of
-// 1024 17.1 / 24.6; 144 of 1024 20.0 / 22.5; 128 rows, 16 of 4096 21.4 / 25.5.  (The flags of the CTAs that gave up in the
-// LSEs, behind one more barrier of the CTA, instead of beside them: 0.4 us more with eight.)
-static int tc_cluster(const specvlm_kv_t* kv, int64_t items, int rows) {
+// their merge.  A cluster costs 7.8 us around its CTAs' tiles, which take 0.7 to 1.3 us each, or around the bytes; slices 13.4
+// (19 with more than 64 rows) around the bytes, with the merge kernel, or around the tiles and ends of a CTA's items.  As many
+// clusters as run side by side: 12 of eight CTAs do and 16 do not, 32 of four and not 36, 72 of two.  Measured, 6 tokens of 8
+// heads per KV head at d = 128, cluster / slices: 8 items of 512 keys 8.6 / 11.3 us, of 4096 12.7 / 14.9, of 16 384 24.6 / 22.7;
+// 32 of 1024 12.5 / 18.8, of 4096 19.5 / 25.9; 64 of 4096 29.1 / 34.4; 96 of 1024 17.1 / 24.6; 144 of 1024 20.0 / 22.5; 128 rows, 16
+// of 4096 21.4 / 25.5; slices of 624 items of 55 / 256 / 1024 35.6 / 46 / 68.  (The flags of the CTAs that gave up in the LSEs,
+// behind one more barrier of the CTA, instead of beside them: 0.4 us more with eight.)
+// *best_us: the estimate.
+static int tc_cluster(const specvlm_kv_t* kv, int64_t items, int rows, double* best_us) {
   const int64_t tiles = (kv->max_seq_len + kBigTokens - 1) / kBigTokens;
-  const double tile_us = kv->head_dim == 128 ? (rows > 64 ? 1.3 : 0.93) : (rows > 64 ? 1.0 : 0.7);
+  const bool wide = kv->head_dim == 128;
+  const double tile_us = wide ? (rows > 64 ? 1.3 : 0.93) : (rows > 64 ? 1.0 : 0.7);
   const double hbm_us = (double)items * kv->max_seq_len * (4.0 * kv->head_dim) / 6.5e6;
+  const double per_cta = (double)items / sm_count();
+  const double work_us = (wide ? 4.3 : 3.1) * (per_cta > 1.0 ? per_cta : 1.0) + 1.1 * tile_us * per_cta * (double)tiles;
   int best = 0;
-  double best_us = (rows > 64 ? 18.0 : 12.3) + hbm_us;
+  *best_us = (rows > 64 ? 19.0 : 13.4) + (work_us > hbm_us ? work_us : hbm_us);
   for (int n = 1; n <= kMaxTcCluster; n *= 2) {
     const int fit = n == 1 ? sm_count() : n == 2 ? 72 : n == 4 ? 32 : 12;
-    const double own_us = tile_us * (double)((tiles + n - 1) / n), us = 7.8 + (own_us > hbm_us ? own_us : hbm_us);
-    if (items <= fit && us < best_us) {
+    const double own_us = tile_us * (double)((tiles + n - 1) / n);
+    const double us = 7.8 + (own_us > hbm_us ? own_us + 0.15 * hbm_us : hbm_us + 0.15 * own_us);
+    if (items <= fit && us < *best_us) {
       best = n;
-      best_us = us;
+      *best_us = us;
     }
   }
   return best;
+}
+
+double attn_tc_window_us(const specvlm_kv_t* kv, int32_t batch, int rows) {
+  double us;
+  tc_cluster(kv, (int64_t)kv->n_layers * batch * kv->n_kv_heads, rows, &us);
+  return us;
 }
 
 // Queries as a 5-D tensor (channel, head in group, query token, KV head, layer * batch + sequence):
@@ -1217,7 +1229,8 @@ int32_t attn_tc_launch(const specvlm_kv_t* kv, const void* q, int32_t batch, int
   if (ws_bytes < attn_tc_ws_bytes(&sched, batch, rows, group)) return SPECVLM_ERR_WORKSPACE_TOO_SMALL;
   if (tree_parents && n_q > kMaxTreeNodes) return SPECVLM_ERR_UNSUPPORTED_SHAPE;
   if (pl.q_per * group > 128) return SPECVLM_ERR_UNSUPPORTED_SHAPE;
-  const int n_parts = pl.n_parts, cluster = win ? tc_cluster(&sched, items, rows) : 0;
+  double us;
+  const int n_parts = pl.n_parts, cluster = win ? tc_cluster(&sched, items, rows, &us) : 0;
   const int ctas = cluster > 0 ? (int)items * cluster : pl.ctas;
 
   CUtensorMap tk, tv;

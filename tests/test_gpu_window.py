@@ -221,13 +221,15 @@ def test_a_page_that_is_needed_and_not_mapped_is_reported():
                 assert int(st) == specvlm.ERR_INVALID_ARG and bool(torch.isfinite(out).all())
 
 
-@pytest.mark.parametrize("L,B,H,Hq,n_q,splits", [(1, 2, 2, 16, 6, 0), (1, 5, 4, 32, 6, 0), (1, 15, 4, 64, 4, 0),
-                                                 (1, 2, 2, 8, 1, 0), (1, 20, 4, 16, 1, 0), (1, 20, 4, 16, 1, 3), (4, 20, 4, 16, 1, 1)])
-def test_what_a_cta_that_gives_up_leaves(L, B, H, Hq, n_q, splits):
-    """Heads that the CTA has a part of keep what was there, the others are whole; the call says so, and the next is not
+@pytest.mark.parametrize("L,B,H,Hq,n_q,splits,W", [
+    (1, 2, 2, 8, 1, 0, 700), (1, 20, 4, 16, 1, 0, 700), (1, 20, 4, 16, 1, 3, 700), (4, 20, 4, 16, 1, 1, 700),       # up to 16 rows
+    (1, 2, 2, 16, 6, 0, 300), (1, 15, 4, 32, 5, 0, 300),                                        # groups of 16 rows
+    (1, 3, 4, 64, 6, 0, 3000), (1, 6, 4, 64, 6, 0, 3000), (1, 15, 4, 64, 6, 0, 3000)])          # clusters on the tensor cores
+def test_what_a_cta_that_gives_up_leaves(L, B, H, Hq, n_q, splits, W):
+    """Rows that the CTA has a part of keep what was there, the others are whole; the call says so, and the next is not
     disturbed."""
-    W, S, D = 700, 70, 128
-    lens = [1000 - 90 * (b % 10) for b in range(B)]
+    S, D, group = 70, 128, Hq // H
+    lens = [W + 300 - 30 * (b % 10) for b in range(B)]
     cache, host = _cache(L, H, D, lens, n_q, W, S, page=64, seed=8)
     q = synth.randn_bf16((L, B, n_q, Hq, D), "cuda", 8, "Q")
     specvlm.debug_set_attn_splits(splits)
@@ -244,11 +246,13 @@ def test_what_a_cta_that_gives_up_leaves(L, B, H, Hq, n_q, splits):
         kept, left = lse == want_lse, lse == 7.0
         assert bool((kept ^ left).all())
         assert torch.equal(out[kept], want[kept]) and bool((out[left] == 7.0).all())
-        whole = left.view(L, B, n_q, H, Hq // H)
-        assert bool((whole == whole[:, :, :1, :, :1]).all())                        # a KV head's rows stand or fall together
-        # one item; on slices the items that the CTA has a part of, and none where it has no work
-        items = int(left.sum()) // (n_q * (Hq // H))
-        assert items == 1 if splits != 3 else items <= 2
+        # a KV head's rows, 16 of them at least, stand or fall together; one item, on slices the items that the CTA has a part of
+        rows = left.view(L, B, n_q, H, group).permute(0, 1, 3, 2, 4).reshape(-1, n_q * group)
+        parts = [p for p in rows.split(16, dim=1)]
+        assert all(bool((p == p[:, :1]).all()) for p in parts)
+        items = int(rows.any(1).sum())
+        lost_parts = sum(int(p[:, 0].sum()) for p in parts)
+        assert (items == 1 and lost_parts in (1, len(parts))) if splits != 3 else items <= 2
         assert int(st) == (specvlm.ERR_TIMEOUT if items else 0) and (items > 0 or lost == n - 1)
 
 
