@@ -565,6 +565,12 @@ int32_t specvlm_debug_wait_timeout(int32_t limit_ms, int32_t* d_status, int32_t*
 void specvlm_debug_set_attn_splits(int32_t n_splits);
 
 /*
+ * Test hook; the paper has no counterpart.  For every later specvlm_window_attn of more than 16 rows per KV head: 1 forces the
+ * tensor cores' kernel, 2 groups of 16 rows on the kernels of up to 16 rows, 0 restores the built-in choice.  Process-wide.
+ */
+void specvlm_debug_set_window_kernel(int32_t mode);
+
+/*
  * Test hook; the paper has no counterpart.  Runs the second kernel of an attention call again, the one that folds the
  * partial results of the (layer, sequence, KV head) items that more than one CTA has worked on, over the
  * scratch that the call left in ws: kv, batch, n_q_heads and ws as in specvlm_draft_decode_attn (n_q = 1) or

@@ -740,6 +740,8 @@ attn_rows16_slices_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid
 // Test hook (specvlm_debug_set_attn_splits): 1 forces a CTA per item, n > 1 slices of about an n-th of a
 // sequence each; 0 leaves the choice to the rule below.
 static std::atomic<int> g_forced_splits{0};
+// Test hook (specvlm_debug_set_window_kernel): 1 the tcgen05 kernel, 2 groups of 16 rows, 0 the rule below
+static std::atomic<int> g_forced_groups{0};
 
 constexpr int kRows16Max = 16;     // windows up to this many rows run on the 16-row kernels
 constexpr int kWindowMaxRows = 128;   // of specvlm_window_attn: what one CTA of the tcgen05 kernel takes
@@ -896,10 +898,11 @@ __global__ void give_up_kernel(const __grid_constant__ AttnTcParams p, int gcta,
 // 12.8; 624 (42 rows) of 55 / 256 37.4 / 50.5 against 35.6 / 46.1, with 21 rows 256 / 1024 35.9 / 77.9 against 44.2 / 68.3; d = 64, 32
 // rows, 448 of 64 / 512 / 1024 11.2 / 21.5 / 33.5 against 24.3 / 31.5 / 38.9.
 static int window_row_groups(const specvlm_kv_t* kv, int32_t batch, int rows) {
-  const int groups = (rows + kRows16Max - 1) / kRows16Max;
+  const int groups = (rows + kRows16Max - 1) / kRows16Max, forced = g_forced_groups.load(std::memory_order_relaxed);
   const int64_t items = (int64_t)kv->n_layers * batch * kv->n_kv_heads, n_groups = items * groups, sms = sm_count();
   const int64_t tiles = (kv->max_seq_len + kTileTokens - 1) / kTileTokens;
-  if ((int64_t)kv->n_layers * batch > 65535 || (int64_t)kv->n_kv_heads * groups > 65535) return 1;
+  if ((int64_t)kv->n_layers * batch > 65535 || (int64_t)kv->n_kv_heads * groups > 65535 || forced == 1) return 1;
+  if (forced == 2) return groups;
   const double hbm_us = (double)items * kv->max_seq_len * (4.0 * kv->head_dim) / 6.5e6;
   double us;
   if (n_groups <= sms) {
@@ -1003,6 +1006,10 @@ using namespace specvlm;
 
 extern "C" void specvlm_debug_set_attn_splits(int32_t n_splits) {
   g_forced_splits.store(n_splits > 0 ? n_splits : 0, std::memory_order_relaxed);
+}
+
+extern "C" void specvlm_debug_set_window_kernel(int32_t mode) {
+  g_forced_groups.store(mode == 1 || mode == 2 ? mode : 0, std::memory_order_relaxed);
 }
 
 extern "C" int32_t specvlm_debug_attn_merge(const specvlm_kv_t* kv, int32_t batch, int32_t n_q_heads, int32_t n_q,

@@ -75,6 +75,7 @@ EXPORTS = [
     "specvlm_compact_pages", "specvlm_debug_poison_shared_memory", "specvlm_debug_wait_timeout",
     "specvlm_debug_set_attn_splits", "specvlm_debug_window_parts", "specvlm_debug_attn_merge",
     "specvlm_debug_attn_give_up", "specvlm_debug_window_give_up",
+    "specvlm_debug_set_window_kernel",
 ]
 
 
@@ -127,6 +128,8 @@ def lib():
         L.specvlm_debug_attn_give_up.restype = c_int32
         L.specvlm_debug_attn_give_up.argtypes = [kvp, c_void_p, c_int32, c_int32, c_float, c_void_p, c_void_p, c_void_p, c_size_t,
                                                  c_int32, i32p, c_void_p, c_void_p]
+        L.specvlm_debug_set_window_kernel.restype = None
+        L.specvlm_debug_set_window_kernel.argtypes = [c_int32]
         L.specvlm_debug_set_attn_splits.restype = None
         L.specvlm_debug_set_attn_splits.argtypes = [c_int32]
         L.specvlm_verify_tree_workspace_bytes.restype = c_size_t
@@ -703,6 +706,12 @@ def debug_set_attn_splits(n_splits: int) -> None:
     """Attention of up to 16 rows per KV head: 1 forces a CTA per (layer, sequence, KV head), more than 1 slices that cut a
     sequence about that many times, 0 is the built-in choice (test hook, process-wide)."""
     lib().specvlm_debug_set_attn_splits(int(n_splits))
+
+
+def debug_set_window_kernel(mode: int) -> None:
+    """window_attn of more than 16 rows per KV head: 1 forces the tensor cores' kernel, 2 groups of 16 rows, 0 is the built-in
+    choice (test hook, process-wide)."""
+    lib().specvlm_debug_set_window_kernel(int(mode))
 
 
 def debug_attn_merge(kv: KvCache, out: torch.Tensor, ws: torch.Tensor, lse: torch.Tensor | None = None,

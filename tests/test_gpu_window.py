@@ -17,6 +17,7 @@ NAN = float("nan")
 def _built_in_choice():
     yield
     specvlm.debug_set_attn_splits(0)
+    specvlm.debug_set_window_kernel(0)
 
 
 def _cache(L, H, D, lens, n_q, window, sinks, *, page, seed, release=True, extra=0):
@@ -94,16 +95,20 @@ def _compare(got, lse, ref):
     assert np.all(np.abs(x[fine] - want[fine]) <= 3e-4 + 2.0 ** -20 * np.abs(want[fine]))
 
 
-def _run(L, Hq, H, D, n_q, lens, window, sinks, *, page=0, seed=0, splits=0, release=True, extra=0):
+def _run(L, Hq, H, D, n_q, lens, window, sinks, *, page=0, seed=0, splits=0, release=True, extra=0, kernels=(1, 2)):
+    """kernels: with more than 16 rows per KV head both the tensor cores and groups of 16 rows, whatever the choice would be."""
     cache, host = _cache(L, H, D, lens, n_q, window, sinks, page=page, seed=seed, release=release, extra=extra)
     q = synth.randn_bf16((L, len(lens), n_q, Hq, D), "cuda", seed, "Q")
-    lse = torch.full(q.shape[:-1], 7.0, dtype=torch.float32, device="cuda")
     st = torch.zeros(1, dtype=torch.int32, device="cuda")
     specvlm.debug_set_attn_splits(splits)
     scale = 1.0 / math.sqrt(D)
-    out = specvlm.window_attn(cache, q, window, sinks, scale, out=torch.full_like(q, NAN), lse=lse, d_status=st)
-    assert int(st) == 0
-    _compare(out, lse, _reference(q, host, lens, window, sinks, scale))
+    ref = _reference(q, host, lens, window, sinks, scale)
+    for kernel in kernels if Hq // H * n_q > 16 else (0,):
+        specvlm.debug_set_window_kernel(kernel)
+        lse = torch.full(q.shape[:-1], 7.0, dtype=torch.float32, device="cuda")
+        out = specvlm.window_attn(cache, q, window, sinks, scale, out=torch.full_like(q, NAN), lse=lse, d_status=st)
+        assert int(st) == 0
+        _compare(out, lse, ref)
 
 
 # (query heads, KV heads, head_dim, n_q): up to 16 rows a KV head, up to 64, up to 128
@@ -145,7 +150,7 @@ def test_sequences_shorter_than_the_window_of_queries(n_q, Hq):
     (1, 130, 4, 1, 64, 1, 100, 3, 64)])
 def test_larger_calls(L, B, Hq, H, D, n_q, window, sinks, page):
     """Calls that the built-in choice gives to clusters, to slices of the tile list, and to the tensor cores."""
-    _run(L, Hq, H, D, n_q, [5000 - 97 * (b % 20) for b in range(B)], window, sinks, page=page, seed=L + B)
+    _run(L, Hq, H, D, n_q, [5000 - 97 * (b % 20) for b in range(B)], window, sinks, page=page, seed=L + B, kernels=(0, 1, 2))
 
 
 @pytest.mark.parametrize("L,B,H", [(1, 2, 1), (1, 3, 4), (1, 5, 4), (2, 8, 2), (3, 11, 2), (1, 20, 5), (4, 20, 2)])
@@ -199,13 +204,15 @@ def test_rising_maxima_across_the_gap():
             host[0][0][:, :, :S] = cache.k[:, blk, :, :S][:, 0].double().cpu().numpy()
             q = synth.randn_bf16((1, 1, n_q, Hq, 128), "cuda", 4, "Q")
             lse = torch.empty(q.shape[:-1], dtype=torch.float32, device="cuda")
-            out = specvlm.window_attn(cache, q, W, S, 0.1, lse=lse)
             ref = _reference(q, host, lens, W, S, 0.1)
             x = np.abs(ref[2]).max()
-            # as _compare, the logits' fp32 sums growing with the factor
-            tol = 2.0 ** -8 * np.abs(ref[0]) * (1 + 2.0 ** -8) + (2.0 ** -8 + 2.0 ** -11 * max(1.0, factor)) * ref[1]
-            assert np.all(np.abs(out.double().cpu().numpy() - ref[0]) <= tol)
-            assert np.abs(lse.double().cpu().numpy() - ref[2]).max() <= 3e-4 * max(1.0, factor) + 2.0 ** -20 * x
+            for kernel in (1, 2):
+                specvlm.debug_set_window_kernel(kernel)
+                out = specvlm.window_attn(cache, q, W, S, 0.1, lse=lse)
+                # as _compare, the logits' fp32 sums growing with the factor
+                tol = 2.0 ** -8 * np.abs(ref[0]) * (1 + 2.0 ** -8) + (2.0 ** -8 + 2.0 ** -11 * max(1.0, factor)) * ref[1]
+                assert np.all(np.abs(out.double().cpu().numpy() - ref[0]) <= tol)
+                assert np.abs(lse.double().cpu().numpy() - ref[2]).max() <= 3e-4 * max(1.0, factor) + 2.0 ** -20 * x
 
 
 def test_a_page_that_is_needed_and_not_mapped_is_reported():
@@ -214,8 +221,9 @@ def test_a_page_that_is_needed_and_not_mapped_is_reported():
             cache, _ = _cache(1, 1, 128, [500, 100], n_q, 200, 5, page=64, seed=5)
             cache.block_table[0, 6] = bad
             q = synth.randn_bf16((1, 2, n_q, Hq, 128), "cuda", 5, "Q")
-            for splits in (0, 1, 3):
+            for splits, kernel in ((0, 1), (1, 2), (3, 0)):
                 specvlm.debug_set_attn_splits(splits)
+                specvlm.debug_set_window_kernel(kernel)
                 st = torch.zeros(1, dtype=torch.int32, device="cuda")
                 out = specvlm.window_attn(cache, q, 200, 5, 0.1, d_status=st)
                 assert int(st) == specvlm.ERR_INVALID_ARG and bool(torch.isfinite(out).all())
