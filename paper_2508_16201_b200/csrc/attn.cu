@@ -6,7 +6,8 @@
 // (cp.async.bulk.tensor) through an mbarrier ring, four warps each score 16 tokens of a tile on
 // m16n8k16 bf16 tiles with a private online softmax, and are merged once per item, i.e. per (layer, sequence, KV
 // head).  An item has a CTA of its own where that is the fastest; else the CTAs work on slices of the list
-// of all tiles.  Windows of more than 16 rows (verification) run on the tcgen05 kernels.
+// of all tiles.  Windows of more than 16 rows (verification) run on the tcgen05 kernels; with a sliding window also here, in groups
+// of 16 rows (window_row_groups).
 #include "attn_tc.cuh"
 
 namespace specvlm {
