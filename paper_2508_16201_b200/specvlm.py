@@ -264,6 +264,9 @@ class KvCache:
         L, NB, H, BT, D = k.shape
         self.dims = (L, H, D)
         self.n_pages = NB
+        # rows of the block table, and whether there is a length for each (for the calls on pages)
+        self.n_rows = block_table.shape[0] if block_table is not None else 0
+        self.lens_for_rows = seq_lens.numel() >= self.n_rows
         s = KvStruct()
         s.k, s.v = k.data_ptr(), v.data_ptr()
         s.stride_layer, s.stride_block, s.stride_head, s.stride_token = (k.stride(0), k.stride(1),
@@ -590,11 +593,9 @@ def pages_workspace_bytes(kv: KvCache, batch: int) -> int:
 
 def _pages(kv: KvCache, ref_count: torch.Tensor) -> int:
     """Checks what the calls on pages share; returns the batch."""
-    assert kv.block_table is not None, "a cache without a block table has no pages"
+    assert kv.n_rows > 0 and kv.lens_for_rows, "a cache without a block table has no pages, and each row of it has a length"
     assert ref_count.dtype is torch.int32 and ref_count.is_contiguous() and ref_count.numel() == kv.n_pages
-    batch = kv.block_table.shape[0]
-    assert kv.seq_lens.numel() >= batch
-    return batch
+    return kv.n_rows
 
 
 def reserve_pages(kv: KvCache, ref_count: torch.Tensor, n_new: int = 0, new_lens: torch.Tensor | None = None,

@@ -88,7 +88,7 @@ class State:
 
 
 @pytest.mark.parametrize("page", [64, 192])
-@pytest.mark.parametrize("pool,batch,L,H,D,unaligned", [(40, 1, 1, 1, 64, False), (61, 3, 2, 2, 128, True), (200, 17, 3, 1, 64, False)])
+@pytest.mark.parametrize("pool,batch,L,H,D,unaligned", [(40, 1, 1, 1, 64, False), (61, 3, 2, 2, 128, True), (200, 17, 3, 1, 64, False), (100, 5, 3, 4, 128, False)])
 def test_branches_share_until_they_write(pool, batch, L, H, D, unaligned, page):
     s = State(pool, page, batch, 3 * page, L=L, H=H, D=D, unaligned=unaligned)
     lens = [(37 * b + 5) % (2 * page) for b in range(batch)]
