@@ -374,8 +374,8 @@ int32_t specvlm_compact_tree_kv(const specvlm_kv_t* kv, const int32_t* path, con
  * not be mapped (specvlm_release_pages).  Rows that some query sees hold finite values.  A block-table entry outside
  * [0, n_blocks) that is needed stands for rows of zeros, and SPECVLM_ERR_INVALID_ARG is stored to d_status.
  * A query that sees no key (seq_len < n_q) gives zeros and an lse of -inf.
- * Supported: head_dim 64/128; group = n_q_heads/n_kv_heads in 1..16 with group * n_q <= 128; batch <= 127 when
- * group * n_q > 16.  Errors and d_status otherwise as for specvlm_verify_attn.
+ * Supported: head_dim 64/128; group = n_q_heads/n_kv_heads in 1..16; batch <= 127 when group * n_q > 16.  Errors and
+ * d_status otherwise as for specvlm_verify_attn.
  */
 size_t specvlm_window_attn_workspace_bytes(const specvlm_kv_t* kv, int32_t batch, int32_t n_q_heads, int32_t n_q,
                                            int32_t window, int32_t n_sinks);

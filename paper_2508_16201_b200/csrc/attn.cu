@@ -745,7 +745,7 @@ static std::atomic<int> g_forced_splits{0};
 static std::atomic<int> g_forced_groups{0};
 
 constexpr int kRows16Max = 16;     // windows up to this many rows run on the 16-row kernels
-constexpr int kWindowMaxRows = 128;   // of specvlm_window_attn: what one CTA of the tcgen05 kernel takes
+constexpr int kTcMaxRows = 128;    // what one CTA of the tcgen05 kernel takes
 
 // Time that one CTA takes for a tile, us.
 static double rows16_tile_us(const specvlm_kv_t* kv) {
@@ -891,19 +891,21 @@ __global__ void give_up_kernel(const __grid_constant__ AttnTcParams p, int gcta,
 }
 
 // Groups of 16 rows that a call with a window and more than 16 rows is cut into for the kernels above, each with CTAs of its own
-// that read the same tiles (all but the first from the L2 cache); 1: none, the tcgen05 kernel.  For short windows and few items the
-// time is what is around the tiles, and that is 4 us here against 8 to 12 there.  Estimated us: 3.9 around the tiles of an item
-// that has an SM, one more for a cluster; beyond, rounds of two CTAs an SM (d = 64: four) with 4.4 around their tiles of 0.75
-// (0.98) each.  Measured, groups / tcgen05, d = 128, 48 rows: 8 items of 64 / 512 / 2048 / 4096 keys 5.1 / 6.3 / 9.2 / 13.3 against
-// 8.7 / 8.6 / 10.6 / 12.9; 32 of 64 / 512 / 1024 5.3 / 8.2 / 11.8 against 9.2 / 10.5 / 12.8; 96 of 64 / 512 6.4 / 11.3 against 9.3 /
-// 12.8; 624 (42 rows) of 55 / 256 37.4 / 50.5 against 35.6 / 46.1, with 21 rows 256 / 1024 35.9 / 77.9 against 44.2 / 68.3; d = 64, 32
-// rows, 448 of 64 / 512 / 1024 11.2 / 21.5 / 33.5 against 24.3 / 31.5 / 38.9.
+// that read the same tiles (all but the first from the L2 cache); 1: none, the tcgen05 kernel, which takes kTcMaxRows rows of a
+// window at most and refuses more.  For short windows and few items the time is what is around the tiles, and that is 4 us here
+// against 8 to 12 there.  Estimated us: 3.9 around the tiles of an item that has an SM, one more for a cluster; beyond, rounds of
+// two CTAs an SM (d = 64: four) with 4.4 around their tiles of 0.75 (0.98) each.  Measured, groups / tcgen05, d = 128, 48 rows: 8
+// items of 64 / 512 / 2048 / 4096 keys 5.1 / 6.3 / 9.2 / 13.3 against 8.7 / 8.6 / 10.6 / 12.9; 32 of 64 / 512 / 1024 5.3 / 8.2 /
+// 11.8 against 9.2 / 10.5 / 12.8; 96 of 64 / 512 6.4 / 11.3 against 9.3 / 12.8; 624 (42 rows) of 55 / 256 37.4 / 50.5 against
+// 35.6 / 46.1, with 21 rows 256 / 1024 35.9 / 77.9 against 44.2 / 68.3; d = 64, 32 rows, 448 of 64 / 512 / 1024 11.2 / 21.5 /
+// 33.5 against 24.3 / 31.5 / 38.9.
 static int window_row_groups(const specvlm_kv_t* kv, int32_t batch, int rows) {
   const int groups = (rows + kRows16Max - 1) / kRows16Max, forced = g_forced_groups.load(std::memory_order_relaxed);
   const int64_t items = (int64_t)kv->n_layers * batch * kv->n_kv_heads, n_groups = items * groups, sms = sm_count();
   const int64_t tiles = (kv->max_seq_len + kTileTokens - 1) / kTileTokens;
-  if ((int64_t)kv->n_layers * batch > 65535 || (int64_t)kv->n_kv_heads * groups > 65535 || forced == 1) return 1;
-  if (forced == 2) return groups;
+  if ((int64_t)kv->n_layers * batch > 65535 || (int64_t)kv->n_kv_heads * groups > 65535) return 1;
+  if (rows > kTcMaxRows || forced == 2) return groups;
+  if (forced == 1) return 1;
   const double hbm_us = (double)items * kv->max_seq_len * (4.0 * kv->head_dim) / 6.5e6;
   double us;
   if (n_groups <= sms) {
@@ -1078,7 +1080,6 @@ extern "C" int32_t specvlm_verify_attn(const specvlm_kv_t* kv, const void* q, in
 extern "C" size_t specvlm_window_attn_workspace_bytes(const specvlm_kv_t* kv, int32_t batch, int32_t n_q_heads, int32_t n_q,
                                                       int32_t window, int32_t n_sinks) {
   if (!kv || n_q < 1 || window < 1 || n_sinks < 0 || kv->n_kv_heads < 1 || kv->max_seq_len < 1) return 0;
-  if ((int64_t)n_q_heads / kv->n_kv_heads * n_q > kWindowMaxRows) return 0;
   const specvlm_kv_t view = KeyWindow(kv, window, n_sinks).view(kv, n_q);
   const size_t bytes = specvlm_attn_workspace_bytes(&view, batch, n_q_heads, n_q - 1);      // 0: refused
   const int rows = bytes > 0 ? n_q_heads / kv->n_kv_heads * n_q : 0;
@@ -1090,7 +1091,7 @@ extern "C" int32_t specvlm_window_attn(const specvlm_kv_t* kv, const void* q, in
                                        void* ws, size_t ws_bytes, int32_t* d_status, void* stream) {
   NvtxRange nvtx_range(__func__);
   if (!kv || window < 1 || n_sinks < 0 || n_q < 1 || kv->n_kv_heads < 1) return SPECVLM_ERR_INVALID_ARG;
-  if (n_q > 9 || (int64_t)n_q_heads / kv->n_kv_heads * n_q > kWindowMaxRows) return SPECVLM_ERR_UNSUPPORTED_SHAPE;
+  if (n_q > 9) return SPECVLM_ERR_UNSUPPORTED_SHAPE;
   const KeyWindow win(kv, window, n_sinks);
   return attn_common(kv, q, batch, n_q_heads, n_q, sm_scale, out, lse_or_null, ws, ws_bytes, d_status, stream, -1, nullptr, &win);
 }
@@ -1100,7 +1101,7 @@ extern "C" int32_t specvlm_debug_window_give_up(const specvlm_kv_t* kv, const vo
                                                 void* ws, size_t ws_bytes, int32_t lost_cta, int32_t* n_ctas, int32_t* d_status,
                                                 void* stream) {
   if (!kv || !n_ctas || window < 1 || n_sinks < 0 || n_q < 1 || kv->n_kv_heads < 1) return SPECVLM_ERR_INVALID_ARG;
-  if (n_q > 9 || (int64_t)n_q_heads / kv->n_kv_heads * n_q > kWindowMaxRows) return SPECVLM_ERR_UNSUPPORTED_SHAPE;
+  if (n_q > 9) return SPECVLM_ERR_UNSUPPORTED_SHAPE;
   const KeyWindow win(kv, window, n_sinks);
   return attn_common(kv, q, batch, n_q_heads, n_q, sm_scale, out, lse_or_null, ws, ws_bytes, d_status, stream, lost_cta, n_ctas, &win);
 }

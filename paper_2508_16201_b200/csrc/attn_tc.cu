@@ -1228,7 +1228,7 @@ int32_t attn_tc_launch(const specvlm_kv_t* kv, const void* q, int32_t batch, int
   const SliceScratch sc = tc_scratch(kv, pl, group);
   if (ws_bytes < attn_tc_ws_bytes(&sched, batch, rows, group)) return SPECVLM_ERR_WORKSPACE_TOO_SMALL;
   if (tree_parents && n_q > kMaxTreeNodes) return SPECVLM_ERR_UNSUPPORTED_SHAPE;
-  if (pl.q_per * group > 128) return SPECVLM_ERR_UNSUPPORTED_SHAPE;
+  if (pl.q_per * group > 128 || (win && pl.n_parts > 1)) return SPECVLM_ERR_UNSUPPORTED_SHAPE;
   double us;
   const int n_parts = pl.n_parts, cluster = win ? tc_cluster(&sched, items, rows, &us) : 0;
   const int ctas = cluster > 0 ? (int)items * cluster : pl.ctas;
@@ -1247,7 +1247,6 @@ int32_t attn_tc_launch(const specvlm_kv_t* kv, const void* q, int32_t batch, int
     p.n_cluster = cluster;
     p.lost_cta = lost_cta;
     if (n_ctas) *n_ctas = cluster > 1 ? ctas : 0;           // (slices have a hook of their own: specvlm_debug_attn_merge)
-    if (n_parts > 1) return SPECVLM_ERR_UNSUPPORTED_SHAPE;
   }
 
   CUtensorMap tq;

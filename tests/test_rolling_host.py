@@ -177,14 +177,14 @@ def test_window_refusals():
     assert call(q=None) == BAD and call(out=None) == BAD and call(q=0x3008) == BAD and call(scale=0.0) == BAD and call(scale=math.nan) == BAD
     assert call(heads=0) == BAD and call(heads=9) == BAD and call(batch=0) == BAD
     assert call(n_q=10) == SHAPE and call(heads=4 * 17) == SHAPE
-    assert call(heads=4 * 16, n_q=9) == SHAPE                                    # 144 rows
     assert call(heads=4 * 8, n_q=6, batch=128) == SHAPE
+    assert call(kv=_with(_kv, n_kv_heads=7300), heads=7300 * 16, n_q=9) == SHAPE   # 144 rows run in groups of 16, as CTAs of a grid
     assert call(heads=4 * 8, n_q=6, ws=None) == BAD and call(heads=4 * 8, n_q=6, ws=0x10010) == BAD
     assert call(heads=4 * 8, n_q=6, size=16) == SMALL
     assert call(kv=_with(_kv, head_dim=96)) == SHAPE and call(kv=_with(_kv, n_kv_heads=0)) == BAD
     size = lambda *a: specvlm.lib().specvlm_window_attn_workspace_bytes(ctypes.byref(_kv()), *a)  # noqa: E731
     assert size(2, 32, 6, 5, 0) > 0 and size(2, 8, 1, 5, 0) > 0
-    for bad in ((0, 8, 1, 5, 0), (2, 8, 0, 5, 0), (2, 8, 1, 0, 0), (2, 8, 1, 5, -1), (2, 64, 9, 5, 0), (2, 9, 1, 5, 0), (2, 8, 10, 5, 0)):
+    for bad in ((0, 8, 1, 5, 0), (2, 8, 0, 5, 0), (2, 8, 1, 0, 0), (2, 8, 1, 5, -1), (2, 68, 1, 5, 0), (2, 9, 1, 5, 0), (2, 8, 10, 5, 0)):
         assert size(*bad) == 0, bad
 
 
