@@ -264,9 +264,11 @@ class KvCache:
         L, NB, H, BT, D = k.shape
         self.dims = (L, H, D)
         self.n_pages = NB
-        # rows of the block table, and whether there is a length for each (for the calls on pages)
+        # rows of the block table, and whether there is a length for each (for the calls on pages); sequences that there are
+        # lengths and rows for
         self.n_rows = block_table.shape[0] if block_table is not None else 0
         self.lens_for_rows = seq_lens.numel() >= self.n_rows
+        self.n_seqs = min(seq_lens.numel(), self.n_rows or NB)
         s = KvStruct()
         s.k, s.v = k.data_ptr(), v.data_ptr()
         s.stride_layer, s.stride_block, s.stride_head, s.stride_token = (k.stride(0), k.stride(1),
@@ -357,7 +359,7 @@ def window_attn(kv: KvCache, q: torch.Tensor, window: int, n_sinks: int, sm_scal
     first ``n_sinks``."""
     L, B, NQ, Hq, D = q.shape
     dims = kv.dims
-    assert q.is_contiguous() and q.dtype is torch.bfloat16 and L == dims[0] and D == dims[2]
+    assert q.is_contiguous() and q.dtype is torch.bfloat16 and L == dims[0] and D == dims[2] and B <= kv.n_seqs
     if out is None:
         out = torch.empty_like(q)
     if ws is None:
@@ -564,7 +566,7 @@ def rope_append_kv(kv: KvCache, rope: Rope, q: torch.Tensor | None, new_k: torch
     shape = new_k.shape
     L, B, n, H, D = shape
     bf16 = torch.bfloat16
-    assert new_k.dtype is bf16 and new_v.dtype is bf16 and new_v.shape == shape and (L, H, D) == kv.dims
+    assert new_k.dtype is bf16 and new_v.dtype is bf16 and new_v.shape == shape and (L, H, D) == kv.dims and B <= kv.n_seqs
     n_q_heads = 0
     if q is not None:
         q_shape = q.shape
