@@ -374,8 +374,8 @@ int32_t specvlm_compact_tree_kv(const specvlm_kv_t* kv, const int32_t* path, con
  * not be mapped (specvlm_release_pages).  Rows that some query sees hold finite values.  A block-table entry outside
  * [0, n_blocks) that is needed stands for rows of zeros, and SPECVLM_ERR_INVALID_ARG is stored to d_status.
  * A query that sees no key (seq_len < n_q) gives zeros and an lse of -inf.
- * Supported: head_dim 64/128; group = n_q_heads/n_kv_heads in 1..16; batch <= 127 when group * n_q > 16.  Errors and
- * d_status otherwise as for specvlm_verify_attn.
+ * Supported: head_dim 64/128; group = n_q_heads/n_kv_heads in 1..16; batch <= 127 when group * n_q > 16; max_seq_len up
+ * to 2^31 - 256.  Errors and d_status otherwise as for specvlm_verify_attn.
  */
 size_t specvlm_window_attn_workspace_bytes(const specvlm_kv_t* kv, int32_t batch, int32_t n_q_heads, int32_t n_q,
                                            int32_t window, int32_t n_sinks);
@@ -440,7 +440,8 @@ int32_t specvlm_rope_frequencies(int32_t scaling, int32_t rot_dim, double base, 
  * Rotates n_new tokens' queries and keys of every sequence and appends keys and values to the cache.  Token t of
  * sequence b goes to cache position start_b + t of every layer and KV head and has positions[a][b][t] on axis a.
  *   kv           host struct of the cache to extend (kv->seq_lens is ignored, see seq_lens_inout)
- *   q, q_out     rows of n_q_heads heads, both or neither (p NULL); q_out may be q itself, else they do not overlap
+ *   q, q_out     rows of n_q_heads heads, both or neither (p NULL); q_out may be q itself, else they do not overlap; no two
+ *                rows of q_out overlap (rows of q, new_k and new_v may: strides of 0)
  *   new_k, new_v rows of kv->n_kv_heads heads; they do not overlap the cache or q_out
  *   positions_or_null  device int32 [n_axes][batch][n_new] (any sign); NULL: start_b + t on every axis
  *   new_lens_or_null   device int32 [batch], 0 .. n_new: sequence b has only that many new tokens, the rows behind them are

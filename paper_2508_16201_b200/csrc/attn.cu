@@ -746,19 +746,20 @@ static std::atomic<int> g_forced_groups{0};
 
 constexpr int kRows16Max = 16;     // windows up to this many rows run on the 16-row kernels
 constexpr int kTcMaxRows = 128;    // what one CTA of the tcgen05 kernel takes
+constexpr int32_t kWindowMaxKeys = 0x7fffff00;     // positions and tiles of a call with a window stay within 31 bits, rounded up too
 
 // Time that one CTA takes for a tile, us.
 static double rows16_tile_us(const specvlm_kv_t* kv) {
   return (kv->head_dim == 128 ? 0.35 : 0.25) * (kv->block_table ? 1.25 : 1.0);
 }
 
-// (window: a call with a window, whose items are all as long as the host's bound.  There 32 clusters of four and 12 of eight, which
-// do run side by side, are used too: 32 items, d = 128, window 512 / 1024 6.53 / 8.45 -> 6.01 / 7.35 us, 12 of 1024 6.56 -> 5.85.)
 // CTAs per item of a launch without slices: the number that is the fastest where every CTA has an SM of its own.  The
 // hand-over costs 1.3 us: one layer of 4 items of 200 tokens 3.7 us with a CTA each, 4.3 with two; of 800 / 1600 / 3200
 // tokens 7.0 / 11.3 / 20.1 with one (7.4 / 8.5 on slices from 1600) and 4.4 / 5.0 / 6.3 with eight.  Clusters do not use
 // every SM of a GPC: 16 of eight CTAs no longer run side by side (4 layers of 800 tokens 7.3 -> 8.4), 24 of four do (2 layers
 // x 3 sequences of 800 tokens 8.0 -> 5.4).
+// window: a call with a window, whose items are all as long as the host's bound.  There 32 clusters of four and 12 of eight, which
+// do run side by side, are used too: 32 items, d = 128, window 512 / 1024 6.53 / 8.45 -> 6.01 / 7.35 us, 12 of 1024 6.56 -> 5.85.
 static int rows16_cluster(const specvlm_kv_t* kv, int64_t items, int64_t tiles, bool window = false) {
   if (g_forced_splits.load(std::memory_order_relaxed) == 1) return 1;
   int best = 1;
@@ -1079,7 +1080,8 @@ extern "C" int32_t specvlm_verify_attn(const specvlm_kv_t* kv, const void* q, in
 
 extern "C" size_t specvlm_window_attn_workspace_bytes(const specvlm_kv_t* kv, int32_t batch, int32_t n_q_heads, int32_t n_q,
                                                       int32_t window, int32_t n_sinks) {
-  if (!kv || n_q < 1 || window < 1 || n_sinks < 0 || kv->n_kv_heads < 1 || kv->max_seq_len < 1) return 0;
+  if (!kv || n_q < 1 || window < 1 || n_sinks < 0 || kv->n_kv_heads < 1 || kv->max_seq_len < 1 || kv->max_seq_len > kWindowMaxKeys)
+    return 0;
   const specvlm_kv_t view = KeyWindow(kv, window, n_sinks).view(kv, n_q);
   const size_t bytes = specvlm_attn_workspace_bytes(&view, batch, n_q_heads, n_q - 1);      // 0: refused
   const int rows = bytes > 0 ? n_q_heads / kv->n_kv_heads * n_q : 0;
@@ -1091,7 +1093,7 @@ extern "C" int32_t specvlm_window_attn(const specvlm_kv_t* kv, const void* q, in
                                        void* ws, size_t ws_bytes, int32_t* d_status, void* stream) {
   NvtxRange nvtx_range(__func__);
   if (!kv || window < 1 || n_sinks < 0 || n_q < 1 || kv->n_kv_heads < 1) return SPECVLM_ERR_INVALID_ARG;
-  if (n_q > 9) return SPECVLM_ERR_UNSUPPORTED_SHAPE;
+  if (n_q > 9 || kv->max_seq_len > kWindowMaxKeys) return SPECVLM_ERR_UNSUPPORTED_SHAPE;
   const KeyWindow win(kv, window, n_sinks);
   return attn_common(kv, q, batch, n_q_heads, n_q, sm_scale, out, lse_or_null, ws, ws_bytes, d_status, stream, -1, nullptr, &win);
 }
@@ -1101,7 +1103,7 @@ extern "C" int32_t specvlm_debug_window_give_up(const specvlm_kv_t* kv, const vo
                                                 void* ws, size_t ws_bytes, int32_t lost_cta, int32_t* n_ctas, int32_t* d_status,
                                                 void* stream) {
   if (!kv || !n_ctas || window < 1 || n_sinks < 0 || n_q < 1 || kv->n_kv_heads < 1) return SPECVLM_ERR_INVALID_ARG;
-  if (n_q > 9) return SPECVLM_ERR_UNSUPPORTED_SHAPE;
+  if (n_q > 9 || kv->max_seq_len > kWindowMaxKeys) return SPECVLM_ERR_UNSUPPORTED_SHAPE;
   const KeyWindow win(kv, window, n_sinks);
   return attn_common(kv, q, batch, n_q_heads, n_q, sm_scale, out, lse_or_null, ws, ws_bytes, d_status, stream, lost_cta, n_ctas, &win);
 }

@@ -255,7 +255,7 @@ __global__ void __launch_bounds__(kPlanThreads) reserve_plan_kernel(const __grid
 // small enough for the cluster's SMs.
 // 64 sequences on 16 384 pages 6.1 -> 3.7 us of the host's time, as long on the device.
 constexpr int kReserveCluster = 8;
-constexpr int64_t kReserveClusterBytes = 4 << 20;
+constexpr double kReserveClusterBytes = 4 << 20;
 __global__ void __launch_bounds__(kPlanThreads) reserve_cluster_kernel(const __grid_constant__ PagesParams p) {
   __shared__ ReservePlan sm;
   pdl_launch_next();
@@ -480,7 +480,7 @@ extern "C" int32_t specvlm_reserve_pages(const specvlm_kv_t* kv, int32_t* block_
   p.n_new = n_new;
   p.new_lens = new_lens_or_null;
   cudaStream_t st = static_cast<cudaStream_t>(stream);
-  const int64_t most_bytes = (int64_t)batch * p.n_layers * p.n_kv_heads * p.block_tokens * kv->head_dim * 4;   // K and V
+  const double most_bytes = (double)batch * p.n_layers * p.n_kv_heads * p.block_tokens * kv->head_dim * 4;   // K and V
   if (most_bytes <= kReserveClusterBytes)
     return launch_clusters_after(reserve_cluster_kernel, dim3(kReserveCluster), kReserveCluster, dim3(kPlanThreads), 0, st, p);
   rc = launch_after(reserve_plan_kernel, dim3(1), dim3(kPlanThreads), 0, st, p);

@@ -177,6 +177,7 @@ def test_window_refusals():
     assert call(q=None) == BAD and call(out=None) == BAD and call(q=0x3008) == BAD and call(scale=0.0) == BAD and call(scale=math.nan) == BAD
     assert call(heads=0) == BAD and call(heads=9) == BAD and call(batch=0) == BAD
     assert call(n_q=10) == SHAPE and call(heads=4 * 17) == SHAPE
+    assert call(kv=_with(_kv, max_seq_len=2 ** 31 - 255, max_blocks=2 ** 25)) == SHAPE
     assert call(heads=4 * 8, n_q=6, batch=128) == SHAPE
     assert call(kv=_with(_kv, n_kv_heads=7300), heads=7300 * 16, n_q=9) == SHAPE   # 144 rows run in groups of 16, as CTAs of a grid
     assert call(heads=4 * 8, n_q=6, ws=None) == BAD and call(heads=4 * 8, n_q=6, ws=0x10010) == BAD
