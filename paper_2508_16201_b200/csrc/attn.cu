@@ -409,9 +409,10 @@ constexpr int kSoloTiles = 4, kSoloTilesPair = 6;
 // (CTAs per SM are as many as the ring allows; without that the compiler held d = 64 to 96 registers and spilled: 6 layers of
 // 800 tokens, 24 items, 4.4 -> 4.2 us, 112 items of d = 128 and 755 tokens 9.83 -> 9.65)
 constexpr int kHalfRing = 4;      // stages of a CTA with two groups that shares an SM with another (d = 64)
+constexpr int kShortRing = 2;     // stages of a CTA that shares an SM with two others (d = 128)
 // WIN: queries see a window and sinks (KeyView); the first tile is not known before the length then.
 template <int D, int STAGES, int NG, bool SPLIT, bool WIN = false>
-__global__ void __launch_bounds__(32 * (4 * NG + 1), NG == 2 ? (STAGES == kHalfRing ? 2 : 1) : D == 64 ? 4 : 2)
+__global__ void __launch_bounds__(32 * (4 * NG + 1), NG == 2 ? (STAGES == kHalfRing ? 2 : 1) : D == 64 ? 4 : STAGES == kShortRing ? 3 : 2)
 attn_rows16_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v,
                    const AttnParams p) {
   constexpr int TILE_BYTES = kTileTokens * D * 2;
@@ -872,6 +873,12 @@ static int32_t launch_rows16(const CUtensorMap& tk, const CUtensorMap& tv, const
   // Short windows, two CTAs an SM: their tiles, one after the other, are the time, and two groups halve them.
   if constexpr (WIN && D == 64)
     if (ctas > sm_count() && ctas <= 2 * sm_count()) return launch_rows16_s<D, kHalfRing, 2, false, WIN>(tk, tv, p, grid, st);
+  // More CTAs than two an SM: windows are mostly short, and a CTA's time what is around its tiles, so three an SM, whose rings are
+  // shorter.  d = 128, two / three: 384 items of 64 / 256 / 512 / 1024 keys 6.2 / 12.9 / 20.8 / 36.1 against 4.4 / 10.8 / 18.1 / 32.4 us, 1088
+  // 14.9 / 28.0 / 46.3 / 84.3 against 13.8 / 26.7 / 46.6 / 86.1.  (d = 64, five of two stages for four of three: 1088 of 64 / 512 keys 6.3 /
+  // 25.3 -> 7.3 / 28.3.)
+  if constexpr (WIN && D == 128)
+    if (ctas > 2 * sm_count()) return launch_rows16_s<D, kShortRing, 1, false, WIN>(tk, tv, p, grid, st);
   return ctas <= sm_count() ? launch_rows16_s<D, kDeep, 2, false, WIN>(tk, tv, p, grid, st)
                             : launch_rows16_s<D, 3, 1, false, WIN>(tk, tv, p, grid, st);
 }
