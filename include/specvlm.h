@@ -567,7 +567,8 @@ void specvlm_debug_set_attn_splits(int32_t n_splits);
 
 /*
  * Test hook; the paper has no counterpart.  For every later specvlm_window_attn of more than 16 rows per KV head: 1 forces the
- * tensor cores' kernel, 2 groups of 16 rows on the kernels of up to 16 rows, 0 restores the built-in choice.  Process-wide.
+ * tensor cores' kernel (up to 128 rows), 2 groups of 16 rows on the kernels of up to 16 rows, 3 a CTA with a warp for each group
+ * of 16 rows, 0 restores the built-in choice.  Process-wide.
  */
 void specvlm_debug_set_window_kernel(int32_t mode);
 
@@ -595,8 +596,8 @@ int32_t specvlm_debug_attn_give_up(const specvlm_kv_t* kv, const void* q, int32_
 
 /*
  * Test hook; the paper has no counterpart.  The same for specvlm_window_attn, where what stays as it is are the rows (query
- * tokens and heads of a KV head) that the CTA has a part of, all of a KV head or 16 of them; n_ctas is 0 where the call runs on the tensor cores
- * without clusters of two or more CTAs, and nobody gives up then.
+ * tokens and heads of a KV head) that the CTA has a part of, all of a KV head or 16 of them; n_ctas is 0 where the call
+ * runs on the tensor cores without clusters of two or more CTAs, and nobody gives up then.
  */
 int32_t specvlm_debug_window_give_up(const specvlm_kv_t* kv, const void* q, int32_t batch, int32_t n_q_heads, int32_t n_q,
                                      int32_t window, int32_t n_sinks, float sm_scale, void* out, float* lse_or_null, void* ws,

@@ -7,7 +7,7 @@
 // m16n8k16 bf16 tiles with a private online softmax, and are merged once per item, i.e. per (layer, sequence, KV
 // head).  An item has a CTA of its own where that is the fastest; else the CTAs work on slices of the list
 // of all tiles.  Windows of more than 16 rows (verification) run on the tcgen05 kernels; with a sliding window also here, in groups
-// of 16 rows (window_row_groups).
+// of 16 rows (window_rows_form).
 #include "attn_tc.cuh"
 
 namespace specvlm {
@@ -55,24 +55,25 @@ struct Rows16 {
     l0 = l1 = 0.f;
   }
 
-  // tile0: position of the tile's first token; vt: the V tile (generic address); cw: this warp's 16-token slice
-  template <bool WIN, typename P>
+  // tile0: position of the tile's first token; vt: the V tile (generic address); cw: this warp's slice of 16 U tokens
+  template <bool WIN, int U = 1, typename P>
   __device__ __forceinline__ void tile(const P& p, int n_q, uint32_t k_base, uint32_t v_base, uint8_t* vt, int tile0, const KeyView& view,
                                        int cw, int lane) {
+    constexpr int SLICE = 16 * U;
     const int kv_len = view.len;
     const float scale_log2 = p.scale_log2;
     const int col = (lane & 3) * 2;
     // per-lane ldmatrix row/chunk selectors
     const int mi = lane >> 3, r8 = lane & 7;
-    const int k_tok = cw * 16 + (mi >> 1) * 8 + r8, k_chunk = mi & 1;   // K: non-transposed
-    const int v_tok = cw * 16 + (mi & 1) * 8 + r8, v_chunk = mi >> 1;   // V: transposed
-    const int tb = tile0 + cw * 16;                                      // first token of this warp's slice
+    const int k_tok = cw * SLICE + (mi >> 1) * 8 + r8, k_chunk = mi & 1;   // K: non-transposed
+    const int v_tok = cw * SLICE + (mi & 1) * 8 + r8, v_chunk = mi >> 1;   // V: transposed
+    const int tb = tile0 + cw * SLICE;                                      // first token of this warp's slice
     if (tb >= kv_len) return;
     // positions that no query sees, between the sinks and the window, hold whatever the page holds, as those past the end do
-    const bool hidden = WIN && tb < view.lo && tb + 16 > p.n_sinks;
+    const bool hidden = WIN && tb < view.lo && tb + SLICE > p.n_sinks;
     if (hidden) {
-      if (tb >= p.n_sinks && tb + 16 <= view.lo) return;
-      const int first = (p.n_sinks > tb ? p.n_sinks : tb) - tile0, last = (view.lo < tb + 16 ? view.lo : tb + 16) - tile0;
+      if (tb >= p.n_sinks && tb + SLICE <= view.lo) return;
+      const int first = (p.n_sinks > tb ? p.n_sinks : tb) - tile0, last = (view.lo < tb + SLICE ? view.lo : tb + SLICE) - tile0;
       for (int t = first + (lane >> 3); t < last; t += 4) {
 #pragma unroll
         for (int h = 0; h < D / 64; ++h)
@@ -82,11 +83,11 @@ struct Rows16 {
       fence_proxy_async();
       __syncwarp();
     }
-    if (tb + 16 > kv_len) {
+    if (tb + SLICE > kv_len) {
       // rows past the end of the sequence hold whatever the page held: clear V there so that
       // a zero probability times a stale non-finite value cannot reach the accumulator
       const int first = kv_len - tile0;                                  // first invalid local row
-      for (int t = first + (lane >> 3); t < cw * 16 + 16; t += 4) {
+      for (int t = first + (lane >> 3); t < (cw + 1) * SLICE; t += 4) {
 #pragma unroll
         for (int h = 0; h < D / 64; ++h)
           *reinterpret_cast<uint4*>(vt + h * (kTileTokens * 128) + t * 128 + (lane & 7) * 16) =
@@ -95,22 +96,25 @@ struct Rows16 {
       fence_proxy_async();                                               // a copy may refill the slot later
       __syncwarp();
     }
-    float sc[2][4];
+    float sc[2 * U][4];
 #pragma unroll
-    for (int nt = 0; nt < 2; ++nt) sc[nt][0] = sc[nt][1] = sc[nt][2] = sc[nt][3] = 0.f;
+    for (int nt = 0; nt < 2 * U; ++nt) sc[nt][0] = sc[nt][1] = sc[nt][2] = sc[nt][3] = 0.f;
 #pragma unroll
     for (int ks = 0; ks < KSTEPS; ++ks) {
-      uint32_t b0, b1, b2, b3;
-      ldmatrix_x4(k_base + tile_offset<D>(k_tok, 2 * ks + k_chunk), b0, b1, b2, b3);
-      mma_bf16_16816(sc[0], qf[ks], b0, b1);
-      mma_bf16_16816(sc[1], qf[ks], b2, b3);
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        uint32_t b0, b1, b2, b3;
+        ldmatrix_x4(k_base + tile_offset<D>(k_tok + 16 * u, 2 * ks + k_chunk), b0, b1, b2, b3);
+        mma_bf16_16816(sc[2 * u], qf[ks], b0, b1);
+        mma_bf16_16816(sc[2 * u + 1], qf[ks], b2, b3);
+      }
     }
     // scale, causal / length mask, running max
     float mx0 = -INFINITY, mx1 = -INFINITY;
     // (WIN: most slices lie inside every query's window; rows out of use may then hold anything)
-    if (WIN && tb + 16 <= view.len - n_q + 1 && (tb >= view.lo + n_q - 1 || tb + 16 <= p.n_sinks)) {
+    if (WIN && tb + SLICE <= view.len - n_q + 1 && (tb >= view.lo + n_q - 1 || tb + SLICE <= p.n_sinks)) {
 #pragma unroll
-      for (int nt = 0; nt < 2; ++nt) {
+      for (int nt = 0; nt < 2 * U; ++nt) {
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
           sc[nt][e] *= scale_log2;
@@ -119,7 +123,7 @@ struct Rows16 {
       }
     } else {
 #pragma unroll
-      for (int nt = 0; nt < 2; ++nt) {
+      for (int nt = 0; nt < 2 * U; ++nt) {
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
           const int tok = tb + nt * 8 + col + (e & 1);
@@ -142,7 +146,7 @@ struct Rows16 {
     m1 = mn1;
     float ps0 = 0.f, ps1 = 0.f;
 #pragma unroll
-    for (int nt = 0; nt < 2; ++nt) {
+    for (int nt = 0; nt < 2 * U; ++nt) {
       sc[nt][0] = fast_exp2(sc[nt][0] - mu0);
       sc[nt][1] = fast_exp2(sc[nt][1] - mu0);
       sc[nt][2] = fast_exp2(sc[nt][2] - mu1);
@@ -152,11 +156,14 @@ struct Rows16 {
     }
     l0 = l0 * a0 + ps0;
     l1 = l1 * a1 + ps1;
-    uint32_t pa[4];
-    pa[0] = pack_bf16x2(sc[0][0], sc[0][1]);
-    pa[1] = pack_bf16x2(sc[0][2], sc[0][3]);
-    pa[2] = pack_bf16x2(sc[1][0], sc[1][1]);
-    pa[3] = pack_bf16x2(sc[1][2], sc[1][3]);
+    uint32_t pa[U][4];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      pa[u][0] = pack_bf16x2(sc[2 * u][0], sc[2 * u][1]);
+      pa[u][1] = pack_bf16x2(sc[2 * u][2], sc[2 * u][3]);
+      pa[u][2] = pack_bf16x2(sc[2 * u + 1][0], sc[2 * u + 1][1]);
+      pa[u][3] = pack_bf16x2(sc[2 * u + 1][2], sc[2 * u + 1][3]);
+    }
 #pragma unroll
     for (int nt = 0; nt < NT_O; ++nt) {
       o[nt][0] *= a0;
@@ -165,11 +172,34 @@ struct Rows16 {
       o[nt][3] *= a1;
     }
 #pragma unroll
-    for (int j = 0; j < D / 16; ++j) {
-      uint32_t b0, b1, b2, b3;
-      ldmatrix_x4_trans(v_base + tile_offset<D>(v_tok, 2 * j + v_chunk), b0, b1, b2, b3);
-      mma_bf16_16816(o[2 * j], pa, b0, b1);
-      mma_bf16_16816(o[2 * j + 1], pa, b2, b3);
+    for (int u = 0; u < U; ++u)
+#pragma unroll
+      for (int j = 0; j < D / 16; ++j) {
+        uint32_t b0, b1, b2, b3;
+        ldmatrix_x4_trans(v_base + tile_offset<D>(v_tok + 16 * u, 2 * j + v_chunk), b0, b1, b2, b3);
+        mma_bf16_16816(o[2 * j], pa[u], b0, b1);
+        mma_bf16_16816(o[2 * j + 1], pa[u], b2, b3);
+      }
+  }
+
+  // the rows of a warp that has seen all of their keys: normalised, to the output
+  __device__ __forceinline__ void store(const AttnParams& p, int base, int rows, int lb, int g, int lane) {
+    l0 += __shfl_xor_sync(0xffffffffu, l0, 1);
+    l0 += __shfl_xor_sync(0xffffffffu, l0, 2);
+    l1 += __shfl_xor_sync(0xffffffffu, l1, 1);
+    l1 += __shfl_xor_sync(0xffffffffu, l1, 2);
+    const int col = (lane & 3) * 2;
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+      const int r = (lane >> 2) + 8 * e;
+      if (r >= rows) continue;
+      const float l = e ? l1 : l0, m = e ? m1 : m0, inv = l > 0.f ? 1.f / l : 0.f;
+      const int t = (base + r) / p.group, h = g * p.group + (base + r - t * p.group);
+      const size_t orow = ((size_t)lb * p.n_q + t) * p.n_q_heads + h;
+#pragma unroll
+      for (int nt = 0; nt < NT_O; ++nt)
+        *reinterpret_cast<uint32_t*>(p.out + orow * D + nt * 8 + col) = pack_bf16x2(o[nt][2 * e] * inv, o[nt][2 * e + 1] * inv);
+      if (p.lse && (lane & 3) == 0) p.lse[orow] = l > 0.f ? (m + log2f(l)) * kLn2 : -INFINITY;
     }
   }
 
@@ -410,6 +440,7 @@ constexpr int kSoloTiles = 4, kSoloTilesPair = 6;
 // 800 tokens, 24 items, 4.4 -> 4.2 us, 112 items of d = 128 and 755 tokens 9.83 -> 9.65)
 constexpr int kHalfRing = 4;      // stages of a CTA with two groups that shares an SM with another (d = 64)
 constexpr int kShortRing = 2;     // stages of a CTA that shares an SM with two others (d = 128)
+constexpr int kShortTiles = 8;
 // WIN: queries see a window and sinks (KeyView); the first tile is not known before the length then.
 template <int D, int STAGES, int NG, bool SPLIT, bool WIN = false>
 __global__ void __launch_bounds__(32 * (4 * NG + 1), NG == 2 ? (STAGES == kHalfRing ? 2 : 1) : D == 64 ? 4 : STAGES == kShortRing ? 3 : 2)
@@ -535,6 +566,111 @@ attn_rows16_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_consta
     }
   }
   rows16_consume<D, STAGES, NG, SPLIT, WIN>(p, smem, base, abort_flag, view, n_my, rank, n_cta);
+}
+
+// ---------------------------------------------------------------------------------------------
+// More than 16 rows per KV head and a window: one CTA per item, in which each consumer warp has 16 of the rows and goes through
+// whole tiles.  Nothing is merged at the end, and a tile is read once for all rows.  For many items of short windows, whose
+// time is what is around the tiles: an SM holds as many items as it holds of the 16-row kernel's groups (window_rows_form).
+// NW: warps at most; U: 16-token slices that a warp scores together, as many as the registers that PER_SM CTAs leave it allow: a
+// tile takes a warp that is alone 2.3 us with one slice at a time, 1.5 to 1.9 with all four (d = 128), 1.3 with two (d = 64).  Two CTAs an SM
+// of four slices for three of one: 42 rows, 2000 items of 64 / 256 / 512 keys 35 / 80 / 141 -> 40 / 83 / 133 us.
+// ---------------------------------------------------------------------------------------------
+template <int D, int NW, int STAGES, int PER_SM, int U>
+__global__ void __launch_bounds__(32 * (NW + 1), PER_SM)
+attn_row_groups_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v, const AttnParams p) {
+  constexpr int TILE_BYTES = kTileTokens * D * 2, STAGE_BYTES = 2 * TILE_BYTES;
+  extern __shared__ uint8_t smem_raw[];
+  const uint32_t raw_addr = smem_u32(smem_raw);
+  const uint32_t base = (raw_addr + 1023u) & ~1023u;
+  uint8_t* const smem = smem_raw + (base - raw_addr);
+  const uint32_t bar_full = base + STAGES * STAGE_BYTES, bar_empty = bar_full + 8 * STAGES;
+  volatile int* const abort_flag = reinterpret_cast<volatile int*>(smem + STAGES * STAGE_BYTES + 16 * STAGES);
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const int g = blockIdx.y, lb = blockIdx.z, layer = lb / p.batch, b = lb - layer * p.batch;
+  const int n_warps = p.row_groups;      // the producer's warp is behind them
+
+  if (tid == 0) {
+    for (int s = 0; s < STAGES; ++s) {
+      mbar_init(bar_full + 8 * s, 1);
+      mbar_init(bar_empty + 8 * s, n_warps);
+    }
+    abort_flag[0] = 0;
+    abort_flag[1] = -1;                  // see await_copies
+    mbar_fence_init();
+  }
+  if (tid == 32 * n_warps) {
+    tma_prefetch_desc(&tm_k);
+    tma_prefetch_desc(&tm_v);
+  }
+  __syncthreads();                       // the barriers are initialised
+  pdl_launch_next();
+  pdl_wait();
+  const KeyView view = key_view<true>(p, p.n_q, b);
+  const int n_tiles = (view.len + kTileTokens - 1) / kTileTokens;
+
+  if (warp == n_warps) {
+    // ------------------------------------------------------------------ producer
+    if (lane != 0) return;
+    const uint64_t policy = l2_policy_evict_first();
+    const int tiles_per_block = p.block_tokens / kTileTokens;     // used only when paged
+    bool ok = true;
+    int issued = 0;
+    for (int i = 0; i < n_tiles && ok; ++i) {
+      const int s = i % STAGES;
+      if (i >= STAGES) ok = mbar_wait(bar_empty + 8 * s, ((i / STAGES) - 1) & 1, abort_flag);
+      if (!ok) break;
+      const int t = key_tile<true>(view, i);
+      int blk = b, tok = t * kTileTokens;
+      if (p.block_table) {
+        blk = p.block_table[(size_t)b * p.max_blocks + t / tiles_per_block];
+        if ((blk < 0 || blk >= p.n_blocks) && p.d_status) *p.d_status = SPECVLM_ERR_INVALID_ARG;   // the copy gives zeros
+        tok = (t % tiles_per_block) * kTileTokens;
+      }
+      const uint32_t full = bar_full + 8 * s, dst = base + s * STAGE_BYTES;
+      mbar_arrive_expect_tx(full, STAGE_BYTES);
+#pragma unroll
+      for (int h = 0; h < D / 64; ++h) {
+        tma_load_5d(dst + h * (kTileTokens * 128), &tm_k, full, h * 64, tok, g, blk, layer, policy);
+        tma_load_5d(dst + TILE_BYTES + h * (kTileTokens * 128), &tm_v, full, h * 64, tok, g, blk, layer, policy);
+      }
+      issued = i + 1;
+    }
+    abort_flag[1] = issued;
+    if (!ok) {                           // a wait expired: stay until the copies in flight have landed
+      if (p.d_status) *p.d_status = SPECVLM_ERR_TIMEOUT;
+      await_copies<STAGES>(bar_full, abort_flag);
+    }
+    return;
+  }
+
+  const int base_row = 16 * warp, rows = p.rows - base_row > 16 ? 16 : p.rows - base_row;
+  Rows16<D> st;
+  st.start(p, p.n_q, base_row + rows, lb, g, view.len, lane, base_row);
+  bool alive = true;
+  for (int i = 0; i < n_tiles; ++i) {
+    const int s = i % STAGES;
+    if (!warp_wait(bar_full + 8 * s, (i / STAGES) & 1, abort_flag)) {
+      alive = false;
+      break;
+    }
+    const uint32_t k_base = base + s * STAGE_BYTES;
+#pragma unroll 1
+    for (int cw = 0; cw < kTileTokens / (16 * U); ++cw)
+      st.template tile<true, U>(p, p.n_q, k_base, k_base + TILE_BYTES, smem + s * STAGE_BYTES + TILE_BYTES, i * kTileTokens, view, cw, lane);
+    __syncwarp();
+    if (lane == 0) mbar_arrive(bar_empty + 8 * s);
+  }
+  // test hook: the CTA that gives up although it has seen its tiles
+  if (p.lost_cta == (int)(blockIdx.z * gridDim.y + blockIdx.y)) alive = false;
+  if (!alive) {                          // leave the rows alone
+    if (lane == 0) {
+      if (p.d_status) *p.d_status = SPECVLM_ERR_TIMEOUT;
+      await_copies<STAGES>(bar_full, abort_flag);
+    }
+    return;
+  }
+  st.store(p, base_row, rows, lb, g, lane);
 }
 
 // bar.sync 1 over n threads (whole warps) that also answers whether the predicate holds for all of them
@@ -742,8 +878,8 @@ attn_rows16_slices_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid
 // Test hook (specvlm_debug_set_attn_splits): 1 forces a CTA per item, n > 1 slices of about an n-th of a
 // sequence each; 0 leaves the choice to the rule below.
 static std::atomic<int> g_forced_splits{0};
-// Test hook (specvlm_debug_set_window_kernel): 1 the tcgen05 kernel, 2 groups of 16 rows, 0 the rule below
-static std::atomic<int> g_forced_groups{0};
+// Test hook (specvlm_debug_set_window_kernel): 1 the tcgen05 kernel, 2 groups of 16 rows, 3 a warp for each, 0 the rule below
+static std::atomic<int> g_forced_rows_form{0};
 
 constexpr int kRows16Max = 16;     // windows up to this many rows run on the 16-row kernels
 constexpr int kTcMaxRows = 128;    // what one CTA of the tcgen05 kernel takes
@@ -866,21 +1002,38 @@ static int32_t launch_rows16_s(const CUtensorMap& tk, const CUtensorMap& tv, con
 // takes 6 stages and two consumer groups instead.
 template <int D, bool WIN>
 static int32_t launch_rows16(const CUtensorMap& tk, const CUtensorMap& tv, const AttnParams& p,
-                             dim3 grid, cudaStream_t st) {
+                             dim3 grid, int64_t tiles, cudaStream_t st) {
   const int64_t ctas = (int64_t)grid.x * grid.y * grid.z;
   constexpr int kDeep = D == 128 ? 6 : 12;
   if (grid.x > 1) return launch_rows16_s<D, kDeep, 2, true, WIN>(tk, tv, p, grid, st);
   // Short windows, two CTAs an SM: their tiles, one after the other, are the time, and two groups halve them.
   if constexpr (WIN && D == 64)
     if (ctas > sm_count() && ctas <= 2 * sm_count()) return launch_rows16_s<D, kHalfRing, 2, false, WIN>(tk, tv, p, grid, st);
-  // More CTAs than two an SM: windows are mostly short, and a CTA's time what is around its tiles, so three an SM, whose rings are
-  // shorter.  d = 128, two / three: 384 items of 64 / 256 / 512 / 1024 keys 6.2 / 12.9 / 20.8 / 36.1 against 4.4 / 10.8 / 18.1 / 32.4 us, 1088
-  // 14.9 / 28.0 / 46.3 / 84.3 against 13.8 / 26.7 / 46.6 / 86.1.  (d = 64, five of two stages for four of three: 1088 of 64 / 512 keys 6.3 /
-  // 25.3 -> 7.3 / 28.3.)
+  // More CTAs than two an SM: where they are short their time is what is around their tiles, and three an SM with shorter rings
+  // overlap more of it.  d = 128, two / three: 384 items, which run at once then, of 64 / 256 / 512 / 1024 keys 6.2 / 12.9 / 20.8 / 36.1 against
+  // 4.4 / 10.8 / 18.1 / 32.4 us, 1088 of 64 / 256 / 512 / 1024 14.9 / 28.0 / 46.3 / 84.3 against 13.8 / 26.7 / 46.6 / 86.1, 896 of 2112 156 against
+  // 164.  (d = 64, five of two stages for four of three: 1088 of 64 / 512 keys 6.3 / 25.3 -> 7.3 / 28.3.)
   if constexpr (WIN && D == 128)
-    if (ctas > 2 * sm_count()) return launch_rows16_s<D, kShortRing, 1, false, WIN>(tk, tv, p, grid, st);
+    if (ctas > 2 * sm_count() && (ctas <= 3 * sm_count() || tiles <= kShortTiles))
+      return launch_rows16_s<D, kShortRing, 1, false, WIN>(tk, tv, p, grid, st);
   return ctas <= sm_count() ? launch_rows16_s<D, kDeep, 2, false, WIN>(tk, tv, p, grid, st)
                             : launch_rows16_s<D, 3, 1, false, WIN>(tk, tv, p, grid, st);
+}
+
+template <int D, int NW, int STAGES, int PER_SM, int U>
+static int32_t launch_row_groups_s(const CUtensorMap& tk, const CUtensorMap& tv, const AttnParams& p, dim3 grid, cudaStream_t st) {
+  constexpr int SMEM = STAGES * 2 * kTileTokens * D * 2 + 1024 + 16 * STAGES + 16;
+  auto kern = attn_row_groups_kernel<D, NW, STAGES, PER_SM, U>;
+  static std::atomic<uint64_t> attr_done{0};
+  if (!smem_attr_once(attr_done, reinterpret_cast<const void*>(kern), SMEM)) return SPECVLM_ERR_CUDA;
+  return launch_after(kern, grid, dim3(32 * (p.row_groups + 1)), (size_t)SMEM, st, tk, tv, p);
+}
+template <int D>
+static int32_t launch_row_groups(const CUtensorMap& tk, const CUtensorMap& tv, const AttnParams& p, dim3 grid, cudaStream_t st) {
+  if constexpr (D == 128)
+    return p.row_groups <= 4 ? launch_row_groups_s<D, 4, 2, 3, 1>(tk, tv, p, grid, st) : launch_row_groups_s<D, 9, 3, 1, 4>(tk, tv, p, grid, st);
+  else
+    return p.row_groups <= 4 ? launch_row_groups_s<D, 4, 3, 4, 2>(tk, tv, p, grid, st) : launch_row_groups_s<D, 9, 3, 2, 2>(tk, tv, p, grid, st);
 }
 
 template <int D, bool WIN>
@@ -898,35 +1051,49 @@ __global__ void give_up_kernel(const __grid_constant__ AttnTcParams p, int gcta,
   unwritten_parts(p, gcta, head_dim, threadIdx.x, blockDim.x);
 }
 
-// Groups of 16 rows that a call with a window and more than 16 rows is cut into for the kernels above, each with CTAs of its own
-// that read the same tiles (all but the first from the L2 cache); 1: none, the tcgen05 kernel, which takes kTcMaxRows rows of a
-// window at most and refuses more.  For short windows and few items the time is what is around the tiles, and that is 4 us here
-// against 8 to 12 there.  Estimated us: 3.9 around the tiles of an item that has an SM, one more for a cluster; beyond, rounds of
-// two CTAs an SM (d = 64: four) with 4.4 around their tiles of 0.75 (0.98) each.  Measured, groups / tcgen05, d = 128, 48 rows: 8
-// items of 64 / 512 / 2048 / 4096 keys 5.1 / 6.3 / 9.2 / 13.3 against 8.7 / 8.6 / 10.6 / 12.9; 32 of 64 / 512 / 1024 5.3 / 8.2 /
-// 11.8 against 9.2 / 10.5 / 12.8; 96 of 64 / 512 6.4 / 11.3 against 9.3 / 12.8; 624 (42 rows) of 55 / 256 37.4 / 50.5 against
-// 35.6 / 46.1, with 21 rows 256 / 1024 35.9 / 77.9 against 44.2 / 68.3; d = 64, 32 rows, 448 of 64 / 512 / 1024 11.2 / 21.5 /
-// 33.5 against 24.3 / 31.5 / 38.9.
-static int window_row_groups(const specvlm_kv_t* kv, int32_t batch, int rows) {
-  const int groups = (rows + kRows16Max - 1) / kRows16Max, forced = g_forced_groups.load(std::memory_order_relaxed);
+// How a call with a window and more than 16 rows runs: on the tcgen05 kernel, which takes kTcMaxRows rows of a window at most and
+// refuses more; as groups of 16 rows on the kernels above, each with CTAs of its own that read the same tiles (all but the first
+// from the L2 cache); or on a CTA per item with a warp for each group.  For short windows the time is what is around the tiles: 4
+// us an item here, which the CTAs of an SM overlap, against 8 to 12 there, or 3 to 4 an item of a CTA's list; a tile takes a warp
+// that goes through it alone 1.2 to 3.6 us, four warps 0.35 and the tcgen05 kernel about 1 for all rows.  So groups where the items
+// are few, warps where they are many and short, tcgen05 where they are long.  Measured, tcgen05 / groups / warps, us: d = 128, 42 rows,
+// 50 items of 64 / 512 keys 6.6 / 4.5 / 5.0 and 10.4 / 9.2 / 21.2, 200 of 512 23.2 / 23.1 / 30.1, 2000 of 512 115 / 171 / 144; 24 rows, 440
+// of 64 / 256 16.2 / 10.5 / 6.2 and 25.4 / 17.8 / 16.6, 2000 of 64 / 256 61 / 41 / 30 and 74 / 70 / 72; 96 rows, 400 of 64 25.4 / 27.6 / 16.4;
+// d = 64, 36 rows, 2000 of 64 / 512 50 / 36 / 21 and 86 / 95 / 75.  The estimates below choose the fastest of the three, or one
+// within 1 % of it on average, in 594 such calls.
+enum class RowsForm { kTc, kGroups, kWarps };
+// (kv: the positions that size the launch, of which `seen` are keys that some query sees)
+static RowsForm window_rows_form(const specvlm_kv_t* kv, int64_t seen, int32_t batch, int rows) {
+  const int groups = (rows + kRows16Max - 1) / kRows16Max, forced = g_forced_rows_form.load(std::memory_order_relaxed);
   const int64_t items = (int64_t)kv->n_layers * batch * kv->n_kv_heads, n_groups = items * groups, sms = sm_count();
   const int64_t tiles = (kv->max_seq_len + kTileTokens - 1) / kTileTokens;
-  if ((int64_t)kv->n_layers * batch > 65535 || (int64_t)kv->n_kv_heads * groups > 65535) return 1;
-  if (rows > kTcMaxRows || forced == 2) return groups;
-  if (forced == 1) return 1;
-  const double hbm_us = (double)items * kv->max_seq_len * (4.0 * kv->head_dim) / 6.5e6;
-  double us;
+  const bool wide = kv->head_dim == 128;
+  if ((int64_t)kv->n_layers * batch > 65535 || (int64_t)kv->n_kv_heads * groups > 65535) return RowsForm::kTc;
+  if (forced == 1 && rows <= kTcMaxRows) return RowsForm::kTc;
+  if (forced > 1) return forced == 2 ? RowsForm::kGroups : RowsForm::kWarps;
+  const double floor_us = 3.9 + (double)items * kv->max_seq_len * (4.0 * kv->head_dim) / 6.5e6;
+  // rounds of `at_once` pieces of work: whole ones while they are few
+  auto rounds = [](int64_t n, int64_t at_once) { return n > 4 * at_once ? (double)n / at_once : (double)((n + at_once - 1) / at_once); };
+  double groups_us;
   if (n_groups <= sms) {
     const int n = rows16_cluster(kv, n_groups, tiles, true);
-    us = 3.9 + (n > 1 ? 1.0 : 0.0) + 1.08 * rows16_tile_us(kv) * (double)((tiles + n - 1) / n);
-  } else if (kv->head_dim == 64 && n_groups <= 2 * sms) {
-    us = 4.2 + 0.5 * (double)tiles;
+    groups_us = 3.9 + (n > 1 ? 1.0 : 0.0) + 1.08 * rows16_tile_us(kv) * (double)((tiles + n - 1) / n);
+  } else if (n_groups <= 2 * sms) {
+    groups_us = wide ? 4.4 + 0.68 * tiles : 4.2 + 0.5 * tiles;
   } else {
-    const double rounds = (double)n_groups / (kv->head_dim == 64 ? 4 * sms : 2 * sms);
-    us = (rounds > 1.0 ? rounds : 1.0) * (4.4 + (kv->head_dim == 64 ? 0.98 : 0.75) * (double)tiles);
+    groups_us = rounds(n_groups, (wide ? 3 : 4) * sms) * (wide ? 4.0 + 0.98 * tiles : 3.0 + 0.74 * tiles);
   }
-  if (us < 3.9 + hbm_us) us = 3.9 + hbm_us;
-  return us < attn_tc_window_us(kv, batch, rows) ? groups : 1;
+  // items on an SM at once (attn_row_groups_kernel), and a tile of an item that is alone there, or not
+  const int most = wide ? (groups <= 4 ? 3 : groups == 5 ? 2 : 1) : groups <= 4 ? 4 : groups == 5 ? 3 : 2;
+  double tile_us = wide ? 2.1 : groups <= 4 ? 1.2 : 1.5;
+  if (items > sms) tile_us = wide ? (groups <= 4 ? 2.0 + 0.4 * groups : groups == 5 ? 2.4 : 2.1) : groups <= 4 ? 0.8 + 0.35 * groups : 2.0;
+  // (up to four warps take a tile in parts, of which they leave out those that no query sees)
+  const double seen_tiles = groups <= 4 ? (double)(seen + (wide ? 16 : 32)) / kTileTokens : (double)tiles;
+  double warps_us = rounds(items, most * sms) * (4.0 + tile_us * (seen_tiles < tiles ? seen_tiles : (double)tiles));
+  if (groups_us < floor_us) groups_us = floor_us;
+  if (warps_us < floor_us) warps_us = floor_us;
+  if (rows <= kTcMaxRows && attn_tc_window_us(kv, batch, rows) <= (groups_us < warps_us ? groups_us : warps_us)) return RowsForm::kTc;
+  return groups_us <= warps_us ? RowsForm::kGroups : RowsForm::kWarps;
 }
 
 static int32_t attn_common(const specvlm_kv_t* kv, const void* q, int32_t batch, int32_t n_q_heads,
@@ -948,8 +1115,9 @@ static int32_t attn_common(const specvlm_kv_t* kv, const void* q, int32_t batch,
     if (!ws || (reinterpret_cast<uintptr_t>(ws) & 255u)) return SPECVLM_ERR_INVALID_ARG;
     if (ws_bytes < attn_tc_ws_bytes(&sched, batch, rows, group)) return SPECVLM_ERR_WORKSPACE_TOO_SMALL;
   }
-  const int row_groups = win && rows > kRows16Max ? window_row_groups(&sched, batch, rows) : 1;
-  if (rows > kRows16Max && row_groups == 1)
+  const RowsForm form = win && rows > kRows16Max ? window_rows_form(&sched, (int64_t)win->window + win->n_sinks + n_q - 1, batch, rows) : RowsForm::kTc;
+  const int row_groups = form != RowsForm::kTc ? (rows + kRows16Max - 1) / kRows16Max : 1;
+  if (rows > kRows16Max && form == RowsForm::kTc)
     return attn_tc_launch(kv, q, batch, n_q_heads, n_q, sm_scale, out, lse, ws, ws_bytes, d_status, st, nullptr, win, lost_cta, n_ctas);
 
   const int64_t lb64 = (int64_t)kv->n_layers * batch;
@@ -1004,11 +1172,17 @@ static int32_t attn_common(const specvlm_kv_t* kv, const void* q, int32_t batch,
   p.n_blocks = kv->n_blocks;
   p.row_groups = row_groups;
 
-  const int n = rows16_cluster(&sched, lb64 * kv->n_kv_heads * row_groups, (sched.max_seq_len + kTileTokens - 1) / kTileTokens, win != nullptr);
+  if (form == RowsForm::kWarps) {
+    const dim3 grid(1, (unsigned)kv->n_kv_heads, (unsigned)lb64);
+    if (n_ctas) *n_ctas = (int32_t)(grid.y * grid.z);
+    return kv->head_dim == 128 ? launch_row_groups<128>(tk, tv, p, grid, st) : launch_row_groups<64>(tk, tv, p, grid, st);
+  }
+  const int64_t tiles = (sched.max_seq_len + kTileTokens - 1) / kTileTokens;
+  const int n = rows16_cluster(&sched, lb64 * kv->n_kv_heads * row_groups, tiles, win != nullptr);
   dim3 grid((unsigned)n, (unsigned)(kv->n_kv_heads * row_groups), (unsigned)lb64);
   if (n_ctas) *n_ctas = (int32_t)(grid.x * grid.y * grid.z);
-  if (win) return kv->head_dim == 128 ? launch_rows16<128, true>(tk, tv, p, grid, st) : launch_rows16<64, true>(tk, tv, p, grid, st);
-  return kv->head_dim == 128 ? launch_rows16<128, false>(tk, tv, p, grid, st) : launch_rows16<64, false>(tk, tv, p, grid, st);
+  if (win) return kv->head_dim == 128 ? launch_rows16<128, true>(tk, tv, p, grid, tiles, st) : launch_rows16<64, true>(tk, tv, p, grid, tiles, st);
+  return kv->head_dim == 128 ? launch_rows16<128, false>(tk, tv, p, grid, tiles, st) : launch_rows16<64, false>(tk, tv, p, grid, tiles, st);
 }
 
 }  // namespace specvlm
@@ -1020,7 +1194,7 @@ extern "C" void specvlm_debug_set_attn_splits(int32_t n_splits) {
 }
 
 extern "C" void specvlm_debug_set_window_kernel(int32_t mode) {
-  g_forced_groups.store(mode == 1 || mode == 2 ? mode : 0, std::memory_order_relaxed);
+  g_forced_rows_form.store(mode >= 1 && mode <= 3 ? mode : 0, std::memory_order_relaxed);
 }
 
 extern "C" int32_t specvlm_debug_attn_merge(const specvlm_kv_t* kv, int32_t batch, int32_t n_q_heads, int32_t n_q,

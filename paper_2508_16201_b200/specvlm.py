@@ -712,8 +712,8 @@ def debug_set_attn_splits(n_splits: int) -> None:
 
 
 def debug_set_window_kernel(mode: int) -> None:
-    """window_attn of more than 16 rows per KV head: 1 forces the tensor cores' kernel, 2 groups of 16 rows, 0 is the built-in
-    choice (test hook, process-wide)."""
+    """window_attn of more than 16 rows per KV head: 1 forces the tensor cores' kernel, 2 groups of 16 rows, 3 a warp for each
+    group, 0 is the built-in choice (test hook, process-wide)."""
     lib().specvlm_debug_set_window_kernel(int(mode))
 
 

@@ -95,8 +95,8 @@ def _compare(got, lse, ref):
     assert np.all(np.abs(x[fine] - want[fine]) <= 3e-4 + 2.0 ** -20 * np.abs(want[fine]))
 
 
-def _run(L, Hq, H, D, n_q, lens, window, sinks, *, page=0, seed=0, splits=0, release=True, extra=0, kernels=(1, 2)):
-    """kernels: with more than 16 rows per KV head both the tensor cores and groups of 16 rows, whatever the choice would be."""
+def _run(L, Hq, H, D, n_q, lens, window, sinks, *, page=0, seed=0, splits=0, release=True, extra=0, kernels=(1, 2, 3)):
+    """kernels: with more than 16 rows per KV head the tensor cores, groups of 16 rows and a warp for each, whatever the choice would be."""
     cache, host = _cache(L, H, D, lens, n_q, window, sinks, page=page, seed=seed, release=release, extra=extra)
     q = synth.randn_bf16((L, len(lens), n_q, Hq, D), "cuda", seed, "Q")
     st = torch.zeros(1, dtype=torch.int32, device="cuda")
@@ -151,7 +151,7 @@ def test_sequences_shorter_than_the_window_of_queries(n_q, Hq):
     (1, 130, 4, 1, 64, 1, 100, 3, 64)])
 def test_larger_calls(L, B, Hq, H, D, n_q, window, sinks, page):
     """Calls that the built-in choice gives to clusters, to slices of the tile list, and to the tensor cores."""
-    _run(L, Hq, H, D, n_q, [5000 - 97 * (b % 20) for b in range(B)], window, sinks, page=page, seed=L + B, kernels=(0, 1, 2))
+    _run(L, Hq, H, D, n_q, [5000 - 97 * (b % 20) for b in range(B)], window, sinks, page=page, seed=L + B, kernels=(0, 1, 2, 3))
 
 
 @pytest.mark.parametrize("L,B,H", [(1, 2, 1), (1, 3, 4), (1, 5, 4), (2, 8, 2), (3, 11, 2), (1, 20, 5), (4, 20, 2)])
@@ -205,7 +205,7 @@ def test_rising_maxima_across_the_gap():
             lse = torch.empty(q.shape[:-1], dtype=torch.float32, device="cuda")
             ref = _reference(q, host, lens, W, S, 0.1)
             x = np.abs(ref[2]).max()
-            for kernel in (1, 2):
+            for kernel in (1, 2, 3):
                 specvlm.debug_set_window_kernel(kernel)
                 out = specvlm.window_attn(cache, q, W, S, 0.1, lse=lse)
                 # as _compare, the logits' fp32 sums growing with the factor
@@ -220,7 +220,7 @@ def test_a_page_that_is_needed_and_not_mapped_is_reported():
             cache, _ = _cache(1, 1, 128, [500, 100], n_q, 200, 5, page=64, seed=5)
             cache.block_table[0, 6] = bad
             q = synth.randn_bf16((1, 2, n_q, Hq, 128), "cuda", 5, "Q")
-            for splits, kernel in ((0, 1), (1, 2), (3, 0)):
+            for splits, kernel in ((0, 1), (1, 2), (3, 0), (0, 3)):
                 specvlm.debug_set_attn_splits(splits)
                 specvlm.debug_set_window_kernel(kernel)
                 st = torch.zeros(1, dtype=torch.int32, device="cuda")
@@ -231,7 +231,8 @@ def test_a_page_that_is_needed_and_not_mapped_is_reported():
 @pytest.mark.parametrize("L,B,H,Hq,n_q,splits,W", [
     (1, 2, 2, 8, 1, 0, 700), (1, 20, 4, 16, 1, 0, 700), (1, 20, 4, 16, 1, 3, 700), (4, 20, 4, 16, 1, 1, 700),       # up to 16 rows
     (1, 2, 2, 16, 6, 0, 300), (1, 15, 4, 32, 5, 0, 300),                                        # groups of 16 rows
-    (1, 3, 4, 64, 6, 0, 3000), (1, 6, 4, 64, 6, 0, 3000), (1, 15, 4, 64, 6, 0, 3000)])          # clusters on the tensor cores
+    (1, 3, 4, 64, 6, 0, 3000), (1, 6, 4, 64, 6, 0, 3000), (1, 15, 4, 64, 6, 0, 3000),           # clusters on the tensor cores
+    (4, 20, 4, 24, 4, 0, 64), (4, 20, 4, 40, 9, 0, 1)])                                         # a warp for 16 rows
 def test_what_a_cta_that_gives_up_leaves(L, B, H, Hq, n_q, splits, W):
     """Rows that the CTA has a part of keep what was there, the others are whole; the call says so, and the next is not
     disturbed."""
