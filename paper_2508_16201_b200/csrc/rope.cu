@@ -119,7 +119,8 @@ __device__ __forceinline__ void turn_sincos(uint32_t turn, float& s, float& c) {
   c = (quarter + 1u) & 2u ? -c : c;
 }
 
-constexpr int kRopeThreads = 128, kRopeOneThreads = 512, kRopeOneTokens = 8;
+constexpr int kRopeThreads = 128, kRopeOneThreads = 512, kRopeOneTokens = 8, kRopeOneCtas = 8;
+constexpr int kRopeOneWarps = kRopeOneCtas * kRopeOneThreads / 32, kRopeOneRounds = 4;
 constexpr int kRopeCtas = 8;                       // on an SM: 64 registers a thread
 constexpr int kRopeWarps = 48;                     // on an SM: with fewer tokens several warps share one
 constexpr int kRopeManyWarps = 128;                // on an SM, that are left where a warp takes several layers
@@ -347,20 +348,22 @@ __device__ __forceinline__ void rope_layers(const RopeParams& p, float* cs_sm, u
   }
 }
 
-// ONE: the only CTA of the launch, which also counts the new tokens
+// ONE: the launch is one CTA, or one cluster, which also counts the new tokens
 template <int D, bool INTER, bool ONE, bool LAYERS = false>
 __global__ void __launch_bounds__(ONE ? kRopeOneThreads : kRopeThreads, ONE ? 1 : kRopeCtas) rope_append_kernel(const __grid_constant__ RopeParams p, uint32_t n_warps) {
   __shared__ __align__(16) float cs_sm[(ONE ? kRopeOneThreads : kRopeThreads) / 32][D];   // cosines and sines of a warp's token
   pdl_launch_next();
   pdl_wait();
-  const uint32_t warp = blockIdx.x * (kRopeThreads / 32) + (threadIdx.x >> 5);
+  const uint32_t warp = blockIdx.x * (blockDim.x >> 5) + (threadIdx.x >> 5);
   if (warp < n_warps) {
     if constexpr (LAYERS) rope_layers<D, INTER>(p, cs_sm[threadIdx.x >> 5], warp, threadIdx.x & 31);
     else rope_rows<D, INTER>(p, cs_sm[threadIdx.x >> 5], warp, threadIdx.x & 31);
   }
   if constexpr (ONE) {
-    __syncthreads();                               // every thread has read the lengths
-    for (int b = threadIdx.x; b < p.batch; b += blockDim.x) rope_count(p, b);
+    if (gridDim.x > 1) cluster_barrier();          // every thread has read the lengths
+    else __syncthreads();
+    if (blockIdx.x == 0)
+      for (int b = threadIdx.x; b < p.batch; b += blockDim.x) rope_count(p, b);
   }
 }
 
@@ -376,9 +379,13 @@ static bool rows_ok(const specvlm_rows_t* r) {
 }
 
 template <int D, bool INTER>
-static int32_t launch_rope(const RopeParams& p, uint32_t n_warps, cudaStream_t st) {
-  if (!p.counted && n_warps <= kRopeOneThreads / 32)
-    return launch_after(rope_append_kernel<D, INTER, true>, dim3(1), dim3(32 * n_warps), 0, st, p, n_warps);
+static int32_t launch_rope(const RopeParams& p, uint32_t n_warps, int one_warps, cudaStream_t st) {
+  if (n_warps <= (uint32_t)one_warps) {
+    int ctas = 1;
+    while (ctas * (kRopeOneThreads / 32) < (int)n_warps) ctas *= 2;
+    return launch_clusters_after(rope_append_kernel<D, INTER, true>, dim3(ctas), ctas, dim3(ctas > 1 ? kRopeOneThreads : 32 * n_warps), 0, st, p,
+                                 n_warps);
+  }
   const uint32_t blocks = (n_warps + kRopeThreads / 32 - 1) / (kRopeThreads / 32);
   const int32_t rc = launch_after(p.per_warp > 0 ? rope_append_kernel<D, INTER, false, true> : rope_append_kernel<D, INTER, false>,
                                   dim3(blocks), dim3(kRopeThreads), 0, st, p, n_warps);
@@ -493,8 +500,14 @@ extern "C" int32_t specvlm_rope_append_kv(const specvlm_kv_t* kv, const specvlm_
   const int64_t rounds = (n_q_heads + rows - 1) / rows + (2 * c.n_kv_heads + rows - 1) / rows, wanted = (int64_t)sm_count() * kRopeWarps;
   int64_t share = (wanted + tokens - 1) / tokens;
   p.share = (int32_t)(share < rounds ? share : rounds);
-  // few tokens that have to be counted: one CTA, which spares the second launch
-  if (!counted && tokens <= kRopeOneTokens && p.share > kRopeOneThreads / 32 / tokens) p.share = (int32_t)(kRopeOneThreads / 32 / tokens);
+  // Few tokens that have to be counted: one CTA or one cluster, which spares the second launch.  17 layers x 6 tokens of 8 + 2 heads, passes
+  // one after the other 11.4 -> 9.5 us, of which 4 are the call; on the device a cluster takes 0.5 us more than two launches, so in a graph,
+  // whose launches cost the host nothing, it is one CTA or none.
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  int one_warps = !counted && tokens <= kRopeOneTokens ? kRopeOneThreads / 32 : 0;
+  if (!counted && one_warps == 0 && tokens <= kRopeOneWarps && rounds <= kRopeOneRounds * (kRopeOneWarps / tokens) && !being_captured(st))
+    one_warps = kRopeOneWarps;
+  if (one_warps > 0 && p.share > one_warps / tokens) p.share = (int32_t)(one_warps / tokens);
   // Many tokens of few rows: a warp takes as many layers as leave four times the warps that the SMs hold (rope_layers; with one
   // layer a warp it still gains, as key and value rows share the queries' rounds).  8 + 2 heads of d = 64, 25 layers of 8723
   // tokens 168 -> 135 us, one of 32 000 27.5 -> 25.6; 4 + 1 heads 28 layers of 8000 163 -> 70, one of 32 000 25.8 -> 21.3.
@@ -502,8 +515,7 @@ extern "C" int32_t specvlm_rope_append_kv(const specvlm_kv_t* kv, const specvlm_
   p.per_warp = (int32_t)(layers < c.n_layers ? layers : c.n_layers);
   const uint32_t n_warps = p.per_warp > 0 ? (uint32_t)((c.n_layers + p.per_warp - 1) / p.per_warp * ((int64_t)batch * n_new))
                                           : (uint32_t)(tokens * p.share);   // < 2^31: more than a warp a token only for few tokens
-  cudaStream_t st = static_cast<cudaStream_t>(stream);
   if (c.head_dim == 128)
-    return rope->interleaved ? launch_rope<128, true>(p, n_warps, st) : launch_rope<128, false>(p, n_warps, st);
-  return rope->interleaved ? launch_rope<64, true>(p, n_warps, st) : launch_rope<64, false>(p, n_warps, st);
+    return rope->interleaved ? launch_rope<128, true>(p, n_warps, one_warps, st) : launch_rope<128, false>(p, n_warps, one_warps, st);
+  return rope->interleaved ? launch_rope<64, true>(p, n_warps, one_warps, st) : launch_rope<64, false>(p, n_warps, one_warps, st);
 }
