@@ -447,9 +447,10 @@ static int32_t pages_params(PagesParams& p, const specvlm_kv_t* kv, int32_t* tab
 }
 
 // CTAs of a launch that copies up to so many pages.  Eight an SM run at once; where most units are there (compaction) CTAs of a
-// unit or a few each, more than run at once, copy faster than ones that walk the list: 900 pages of 28 layers x 4 heads, a
-// quarter of them moved, 257 us of copying with 8 an SM, 241 with 64 (6.5 TB/s of bytes moved); a reservation seldom copies
-// anything, and its CTAs are few.
+// unit or a few each, more than run at once, copy faster than ones that walk the list, but those that find nothing to move cost a
+// nanosecond each: 900 pages of 28 layers x 4 heads, a quarter of them moved, 8 / 16 / 32 / 64 an SM 258 / 253 / 248 / 246 us (6.4 TB/s of
+// bytes moved in the kernel), 705 of 8 x 2 18.5 / 19.3 / 20.0 / 21.1, nothing of 117 of 22 x 8 7.2 / 8.2 / 10.8 / 15.9; a reservation seldom
+// copies anything, and its CTAs are few.
 static unsigned copy_grid(const PagesParams& p, int64_t most_copies, int ctas_per_sm) {
   const int64_t units = most_copies * p.n_layers * p.n_kv_heads, cap = (int64_t)sm_count() * ctas_per_sm;
   return (unsigned)(units < cap ? units : cap);
@@ -526,5 +527,5 @@ extern "C" int32_t specvlm_compact_pages(const specvlm_kv_t* kv, int32_t* block_
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   rc = launch_after(compact_plan_kernel, dim3(1), dim3(kPlanThreads), 0, st, p);
   if (rc != SPECVLM_OK) return rc;
-  return launch_after(compact_move_kernel, dim3(copy_grid(p, (p.n_blocks + 1) / 2, 64)), dim3(kCopyThreads), 0, st, p);
+  return launch_after(compact_move_kernel, dim3(copy_grid(p, (p.n_blocks + 1) / 2, 32)), dim3(kCopyThreads), 0, st, p);
 }
