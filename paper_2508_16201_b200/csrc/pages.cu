@@ -446,14 +446,15 @@ static int32_t pages_params(PagesParams& p, const specvlm_kv_t* kv, int32_t* tab
   return SPECVLM_OK;
 }
 
-// CTAs of a launch that copies up to so many pages.  Eight an SM run at once; where most units are there (compaction) CTAs of a
-// unit or a few each, more than run at once, copy faster than ones that walk the list, but those that find nothing to move cost a
-// nanosecond each: 900 pages of 28 layers x 4 heads, a quarter of them moved, 8 / 16 / 32 / 64 an SM 258 / 253 / 248 / 246 us (6.4 TB/s of
-// bytes moved in the kernel), 705 of 8 x 2 18.5 / 19.3 / 20.0 / 21.1, nothing of 117 of 22 x 8 7.2 / 8.2 / 10.8 / 15.9; a reservation seldom
-// copies anything, and its CTAs are few.
-static unsigned copy_grid(const PagesParams& p, int64_t most_copies, int ctas_per_sm) {
-  const int64_t units = most_copies * p.n_layers * p.n_kv_heads, cap = (int64_t)sm_count() * ctas_per_sm;
-  return (unsigned)(units < cap ? units : cap);
+// CTAs of a launch that copies up to so many pages, for `units_each` units of them at least, but eight an SM, which run at once.
+// Where most units are there (compaction) CTAs of a unit or a few each, more than run at once, copy faster than ones that walk the
+// list, but those that find nothing to move cost a nanosecond each: 900 pages of 28 layers x 4 heads, a quarter of them moved, 8 /
+// 16 / 32 / 64 an SM 258 / 253 / 248 / 246 us (6.4 TB/s of bytes moved in the kernel), 705 of 8 x 2 18.5 / 19.3 / 20.0 / 21.1, 30 of 117 pages of
+// 22 x 8 64.8 / 62.8 / 61.8 / 61.9, none of them 7.2 / 8.2 / 10.8 / 15.9.  A reservation seldom copies anything, and its CTAs are few.
+static unsigned copy_grid(const PagesParams& p, int64_t most_copies, int units_each, int most_per_sm) {
+  const int64_t units = most_copies * p.n_layers * p.n_kv_heads, few = 8 * (int64_t)sm_count(), cap = (int64_t)sm_count() * most_per_sm;
+  const int64_t n = units < few ? units : units / units_each > few ? units / units_each : few;
+  return (unsigned)(n < cap ? n : cap);
 }
 
 static bool overlap(const void* a, size_t a_bytes, const void* b, size_t b_bytes) {
@@ -486,7 +487,7 @@ extern "C" int32_t specvlm_reserve_pages(const specvlm_kv_t* kv, int32_t* block_
     return launch_clusters_after(reserve_cluster_kernel, dim3(kReserveCluster), kReserveCluster, dim3(kPlanThreads), 0, st, p);
   rc = launch_after(reserve_plan_kernel, dim3(1), dim3(kPlanThreads), 0, st, p);
   if (rc != SPECVLM_OK) return rc;
-  return launch_after(copy_pages_kernel, dim3(copy_grid(p, batch, 8)), dim3(kCopyThreads), 0, st, p);
+  return launch_after(copy_pages_kernel, dim3(copy_grid(p, batch, 1, 8)), dim3(kCopyThreads), 0, st, p);
 }
 
 extern "C" int32_t specvlm_release_pages(const specvlm_kv_t* kv, int32_t* block_table_inout, int32_t* ref_count_inout,
@@ -527,5 +528,5 @@ extern "C" int32_t specvlm_compact_pages(const specvlm_kv_t* kv, int32_t* block_
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   rc = launch_after(compact_plan_kernel, dim3(1), dim3(kPlanThreads), 0, st, p);
   if (rc != SPECVLM_OK) return rc;
-  return launch_after(compact_move_kernel, dim3(copy_grid(p, (p.n_blocks + 1) / 2, 32)), dim3(kCopyThreads), 0, st, p);
+  return launch_after(compact_move_kernel, dim3(copy_grid(p, (p.n_blocks + 1) / 2, 3, 64)), dim3(kCopyThreads), 0, st, p);
 }
