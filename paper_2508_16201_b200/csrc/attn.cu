@@ -269,6 +269,8 @@ __device__ __forceinline__ void store_bf16x4(__nv_bfloat16* dst, const float4& v
 }
 
 constexpr int kMaxRows16Cluster = 8;       // the portable cluster size
+constexpr int kSliceTokens = 16;           // of a tile that is copied in slices (load_seen)
+constexpr int kSlicedTiles = 3;            // in windows of at most so many
 
 // By a consumer thread of a CTA that gives up (a wait expired): it stays, bounded, until the producer has gone and the last
 // copies that it asked for have landed, since the CTA must not end under copies to its shared memory.  flags[0] is the abort
@@ -281,6 +283,31 @@ __device__ __forceinline__ void await_copies(uint32_t bar_full, volatile int* fl
   const int issued = flags[1];
   for (int i = issued > STAGES ? issued - STAGES : 0; i < issued; ++i)
     while (!mbar_try_wait(bar_full + 8 * (i % STAGES), (i / STAGES) & 1) && global_timer_ns() - t0 < kWaitLimitNs) {
+    }
+}
+
+// The copies of a window's tile at position tile0 in slices of 16 tokens (kSliceTokens), those that no query sees left out.
+template <int D>
+__device__ __forceinline__ void load_seen(const CUtensorMap& tm_k, const CUtensorMap& tm_v, const KeyView& view, int n_sinks, int tile0, uint32_t dst,
+                                          uint32_t full, int tok, int g, int blk, int layer, uint64_t policy) {
+  constexpr int TILE_BYTES = kTileTokens * D * 2, N = kTileTokens / kSliceTokens;
+  auto seen = [&](int u) {
+    const int at = tile0 + u * kSliceTokens;
+    return at < view.len && (at < n_sinks || at + kSliceTokens > view.lo);
+  };
+  int n = 0;
+#pragma unroll
+  for (int u = 0; u < N; ++u) n += seen(u);
+  mbar_arrive_expect_tx(full, n * (2 * TILE_BYTES / N));
+#pragma unroll
+  for (int u = 0; u < N; ++u)
+    if (seen(u)) {
+#pragma unroll
+      for (int h = 0; h < D / 64; ++h) {
+        const uint32_t at = dst + h * (kTileTokens * 128) + u * (kSliceTokens * 128);
+        tma_load_5d(at, &tm_k, full, h * 64, tok + u * kSliceTokens, g, blk, layer, policy);
+        tma_load_5d(at + TILE_BYTES, &tm_v, full, h * 64, tok + u * kSliceTokens, g, blk, layer, policy);
+      }
     }
 }
 
@@ -533,8 +560,13 @@ attn_rows16_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_consta
           tok = t * kTileTokens;
         }
         const uint32_t full = bar_full + 8 * s;
-        mbar_arrive_expect_tx(full, STAGE_BYTES);
         const uint32_t dst = base + s * STAGE_BYTES;
+        if (WIN && !SPLIT && p.sliced) {
+          load_seen<D>(tm_k, tm_v, view, p.n_sinks, i * kTileTokens, dst, full, tok, g, blk, layer, policy);
+          issued = i + 1;
+          continue;
+        }
+        mbar_arrive_expect_tx(full, STAGE_BYTES);
 #pragma unroll
         for (int h = 0; h < D / 64; ++h) {
           tma_load_5d(dst + h * (kTileTokens * 128), &tm_k, full, h * 64, tok, g, blk, layer, policy);
@@ -628,6 +660,11 @@ attn_row_groups_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_co
         tok = (t % tiles_per_block) * kTileTokens;
       }
       const uint32_t full = bar_full + 8 * s, dst = base + s * STAGE_BYTES;
+      if (p.sliced) {
+        load_seen<D>(tm_k, tm_v, view, p.n_sinks, i * kTileTokens, dst, full, tok, g, blk, layer, policy);
+        issued = i + 1;
+        continue;
+      }
       mbar_arrive_expect_tx(full, STAGE_BYTES);
 #pragma unroll
       for (int h = 0; h < D / 64; ++h) {
@@ -1122,18 +1159,26 @@ static int32_t attn_common(const specvlm_kv_t* kv, const void* q, int32_t batch,
 
   const int64_t lb64 = (int64_t)kv->n_layers * batch;
   if (lb64 > 65535 || kv->n_kv_heads * row_groups > 65535) return SPECVLM_ERR_UNSUPPORTED_SHAPE;
-  CUtensorMap tk, tv;
-  rc = encode_kv_map(&tk, kv, kv->k, kTileTokens);
-  if (rc != SPECVLM_OK) return rc;
-  rc = encode_kv_map(&tv, kv, kv->v, kTileTokens);
-  if (rc != SPECVLM_OK) return rc;
-
   int scratch_ctas = 0;
   const int ctas = row_groups > 1 ? 0 : rows16_slices(&sched, batch, &scratch_ctas, win != nullptr);
   if (scratch_ctas > 0) {
     if (!ws || (reinterpret_cast<uintptr_t>(ws) & 255u)) return SPECVLM_ERR_INVALID_ARG;
     if (ws_bytes < rows16_scratch_bytes(kv, scratch_ctas, rows)) return SPECVLM_ERR_WORKSPACE_TOO_SMALL;
   }
+  const int64_t tiles = (sched.max_seq_len + kTileTokens - 1) / kTileTokens, items = lb64 * kv->n_kv_heads * (form == RowsForm::kWarps ? 1 : row_groups);
+  const int n = ctas > 0 || form == RowsForm::kWarps ? 1 : rows16_cluster(&sched, items, tiles, win != nullptr);
+  // The tiles of short windows are mostly rows that no query sees.  Where there are more CTAs than SMs these need not be read: copies of
+  // 16 rows.  A wait for twelve of them takes longer than for four of 64 where the CTAs are few.  Windows of 16 / 100 / 400 keys, whole
+  // tiles / slices, us, d = 128: 48 items 3.4 / 4.3 / - against 3.3 / 5.0 / -, 200 4.0 / 6.7 / - against 3.6 / 5.7 / -, 1088 12.8 / 22.5 / 41.8
+  // against 10.6 / 20.5 / 42.4, of 50 keys and 4 sinks 22.6 against 18.5; 24 rows, a warp for 16, 18.6 / 27.7 / 67.3 against 15.4 / 26.5 / 65.4.
+  const bool sliced = win && ctas == 0 && n == 1 && tiles <= kSlicedTiles && sched.max_seq_len < kv->max_seq_len &&
+                      2 * items > (kv->head_dim == 128 ? 2 : 3) * (int64_t)sm_count();
+  CUtensorMap tk, tv;
+  rc = encode_kv_map(&tk, kv, kv->k, sliced ? kSliceTokens : kTileTokens);
+  if (rc != SPECVLM_OK) return rc;
+  rc = encode_kv_map(&tv, kv, kv->v, sliced ? kSliceTokens : kTileTokens);
+  if (rc != SPECVLM_OK) return rc;
+
   if (ctas > 0) {
     const SliceScratch sc(ctas, rows, kv->head_dim);
     AttnTcParams p = slice_params(kv, q, batch, n_q_heads, n_q, sm_scale, out, lse, d_status, 1, n_q, ws, sc);
@@ -1171,14 +1216,13 @@ static int32_t attn_common(const specvlm_kv_t* kv, const void* q, int32_t batch,
   p.n_sinks = win ? win->n_sinks : 0;
   p.n_blocks = kv->n_blocks;
   p.row_groups = row_groups;
+  p.sliced = sliced ? 1 : 0;
 
   if (form == RowsForm::kWarps) {
     const dim3 grid(1, (unsigned)kv->n_kv_heads, (unsigned)lb64);
     if (n_ctas) *n_ctas = (int32_t)(grid.y * grid.z);
     return kv->head_dim == 128 ? launch_row_groups<128>(tk, tv, p, grid, st) : launch_row_groups<64>(tk, tv, p, grid, st);
   }
-  const int64_t tiles = (sched.max_seq_len + kTileTokens - 1) / kTileTokens;
-  const int n = rows16_cluster(&sched, lb64 * kv->n_kv_heads * row_groups, tiles, win != nullptr);
   dim3 grid((unsigned)n, (unsigned)(kv->n_kv_heads * row_groups), (unsigned)lb64);
   if (n_ctas) *n_ctas = (int32_t)(grid.x * grid.y * grid.z);
   if (win) return kv->head_dim == 128 ? launch_rows16<128, true>(tk, tv, p, grid, tiles, st) : launch_rows16<64, true>(tk, tv, p, grid, tiles, st);

@@ -18,6 +18,7 @@ struct AttnParams {
   int32_t window, n_sinks;    // specvlm_window_attn: the last keys and the first keys that a query sees
   int32_t n_blocks;           // pages of the cache
   int32_t row_groups;         // with a window, and more than 16 rows per KV head: groups of 16 rows, an item each
+  int32_t sliced;             // with a window: tiles are copied in slices, without those that no query sees
 };
 
 __device__ __forceinline__ int clamp_len(int n, int max_len) { return n < 0 ? 0 : (n > max_len ? max_len : n); }

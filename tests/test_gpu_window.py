@@ -163,6 +163,14 @@ def test_items_of_every_number(L, B, H, Hq, D, n_q):
     _run(L, Hq * H, H, D, n_q, lens, 260, 70, page=64, seed=B)
 
 
+@pytest.mark.parametrize("Hq,D,n_q", [(7, 128, 1), (4, 64, 2), (8, 128, 4), (16, 128, 9), (9, 64, 9)])
+@pytest.mark.parametrize("window,sinks,page", [(1, 0, 64), (16, 33, 0), (50, 4, 128), (62, 64, 64), (121, 0, 0)])
+def test_many_items_of_short_windows(Hq, D, n_q, window, sinks, page):
+    """280 items of three tiles at most, whose copies leave out the slices that no query sees."""
+    lens = [0, 1, 15, 16, 17, 40, 63, 64, 65, 100, 127, 128, 129, 150, 190, 191, 192, 193, 300, 333, 350, 400, 555, 600, 640, 700, 701, 777]
+    _run(5, Hq * 2, 2, D, n_q, lens, window, sinks, page=page, seed=window, kernels=(0, 2, 3))
+
+
 @pytest.mark.parametrize("seed", range(40))
 def test_random_windows(seed):
     rng = np.random.default_rng(1000 + seed)
