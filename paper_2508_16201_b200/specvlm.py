@@ -355,13 +355,18 @@ def window_attn_workspace_bytes(kv: KvCache, batch: int, n_q_heads: int, n_q: in
 def window_attn(kv: KvCache, q: torch.Tensor, window: int, n_sinks: int, sm_scale: float, out: torch.Tensor | None = None,
                 lse: torch.Tensor | None = None, ws: torch.Tensor | None = None,
                 d_status: torch.Tensor | None = None) -> torch.Tensor:
-    """q, out: bf16 [n_layers][batch][n_q][n_q_heads][head_dim]; a query sees the last ``window`` keys up to its own and the
-    first ``n_sinks``."""
-    L, B, NQ, Hq, D = q.shape
+    """q, out: bf16 [n_layers][batch][n_q][n_q_heads][head_dim], lse: fp32 [n_layers][batch][n_q][n_q_heads], all contiguous; a
+    query sees the last ``window`` keys up to its own and the first ``n_sinks``."""
+    shape = q.shape
+    L, B, NQ, Hq, D = shape
     dims = kv.dims
     assert q.is_contiguous() and q.dtype is torch.bfloat16 and L == dims[0] and D == dims[2] and B <= kv.n_seqs
     if out is None:
         out = torch.empty_like(q)
+    else:
+        assert out.dtype is torch.bfloat16 and out.shape == shape and out.is_contiguous()
+    if lse is not None:
+        assert lse.dtype is torch.float32 and lse.shape == shape[:-1] and lse.is_contiguous()
     if ws is None:
         ws = _ws(window_attn_workspace_bytes(kv, B, Hq, NQ, window, n_sinks), q.device)
     rc = native().window_attn(addressof(kv.struct), q, B, Hq, NQ, window, n_sinks, float(sm_scale), out, lse, ws, ws.numel(),
