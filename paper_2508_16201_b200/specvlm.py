@@ -250,15 +250,15 @@ class KvCache:
     """A bf16 K/V cache in device memory plus its specvlm_kv_t descriptor.
 
     ``k``/``v``: tensors of shape [n_layers][n_blocks][n_kv_heads][block_tokens][head_dim]
-    (any strides with a unit channel stride).  ``block_table`` None = contiguous: sequence b
-    is block b.
+    (any strides with a unit channel stride).  ``seq_lens``: int32, contiguous.  ``block_table``
+    None = contiguous: sequence b is block b.
     """
 
     def __init__(self, k: torch.Tensor, v: torch.Tensor, seq_lens: torch.Tensor, max_seq_len: int,
                  block_table: torch.Tensor | None = None):
         assert k.dtype == torch.bfloat16 and v.dtype == torch.bfloat16 and k.dim() == 5
         assert k.shape == v.shape and k.stride() == v.stride() and k.stride(4) == 1
-        assert seq_lens.dtype == torch.int32
+        assert seq_lens.dtype == torch.int32 and seq_lens.is_contiguous()
         self.k, self.v, self.seq_lens, self.block_table = k, v, seq_lens, block_table
         self.max_seq_len = int(max_seq_len)
         L, NB, H, BT, D = k.shape

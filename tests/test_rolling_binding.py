@@ -60,3 +60,13 @@ def test_window_lse_that_does_not_fit_is_refused(native, lse):
     with pytest.raises(AssertionError):
         _window(lse=lse)
     assert native.calls == []
+
+
+def test_strided_lengths_are_refused():
+    """Lengths are read, and by the append written, one after the other."""
+    lens = torch.zeros((2, 2), dtype=I32)
+    assert _cache(lens[0]).struct.seq_lens == lens.data_ptr() and _cache(torch.zeros(4, dtype=I32)).n_seqs == 2
+    for bad in (lens[:, 0], torch.zeros(1, dtype=I32).expand(2), torch.zeros(4, dtype=I32)[::2]):
+        for paged in (False, True):
+            with pytest.raises(AssertionError):
+                _cache(bad, paged)
