@@ -238,6 +238,14 @@ def _stream():
     return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
 
 
+_I32_MAX = 0x7fffffff
+
+
+def _within_i32(x):
+    """A number of tokens for a 32-bit argument, which the conversion would take modulo 2^32: one beyond is as good as the largest."""
+    return x if -_I32_MAX <= x <= _I32_MAX else _I32_MAX if x > 0 else -_I32_MAX
+
+
 _i32_types = [c_int32 * n for n in range(130)]      # array types of the usual batch sizes
 
 
@@ -349,7 +357,8 @@ def verify_attn(kv: KvCache, q: torch.Tensor, gamma: int, sm_scale: float,
 
 
 def window_attn_workspace_bytes(kv: KvCache, batch: int, n_q_heads: int, n_q: int, window: int, n_sinks: int) -> int:
-    return int(lib().specvlm_window_attn_workspace_bytes(byref(kv.struct), batch, n_q_heads, n_q, window, n_sinks))
+    return int(lib().specvlm_window_attn_workspace_bytes(byref(kv.struct), batch, n_q_heads, n_q, _within_i32(window),
+                                                           _within_i32(n_sinks)))
 
 
 def window_attn(kv: KvCache, q: torch.Tensor, window: int, n_sinks: int, sm_scale: float, out: torch.Tensor | None = None,
@@ -369,8 +378,8 @@ def window_attn(kv: KvCache, q: torch.Tensor, window: int, n_sinks: int, sm_scal
         assert lse.dtype is torch.float32 and lse.shape == shape[:-1] and lse.is_contiguous()
     if ws is None:
         ws = _ws(window_attn_workspace_bytes(kv, B, Hq, NQ, window, n_sinks), q.device)
-    rc = native().window_attn(addressof(kv.struct), q, B, Hq, NQ, window, n_sinks, float(sm_scale), out, lse, ws, ws.numel(),
-                              d_status)
+    rc = native().window_attn(addressof(kv.struct), q, B, Hq, NQ, _within_i32(window), _within_i32(n_sinks), float(sm_scale), out, lse,
+                              ws, ws.numel(), d_status)
     if rc:
         _check(rc, "specvlm_window_attn")
     return out
@@ -613,7 +622,8 @@ def reserve_pages(kv: KvCache, ref_count: torch.Tensor, n_new: int = 0, new_lens
         assert new_lens.dtype == torch.int32 and new_lens.is_contiguous() and new_lens.numel() == B
     if ws is None:
         ws = _ws(pages_workspace_bytes(kv, B), ref_count.device)
-    rc = native().reserve_pages(addressof(kv.struct), kv.block_table, ref_count, B, n_new, new_lens, ws, ws.numel(), d_status)
+    rc = native().reserve_pages(addressof(kv.struct), kv.block_table, ref_count, B, _within_i32(n_new), new_lens, ws, ws.numel(),
+                                d_status)
     if rc:
         _check(rc, "specvlm_reserve_pages")
 
@@ -622,8 +632,8 @@ def release_pages(kv: KvCache, ref_count: torch.Tensor, window: int | None = Non
                   d_status: torch.Tensor | None = None) -> None:
     """Gives back the pages without a row that is still needed; kv.block_table and ref_count are updated."""
     B = _pages(kv, ref_count)
-    rc = native().release_pages(addressof(kv.struct), kv.block_table, ref_count, B, 0x7fffffff if window is None else window,
-                                n_sinks, d_status)
+    rc = native().release_pages(addressof(kv.struct), kv.block_table, ref_count, B, _I32_MAX if window is None else _within_i32(window),
+                                _within_i32(n_sinks), d_status)
     if rc:
         _check(rc, "specvlm_release_pages")
 

@@ -70,3 +70,32 @@ def test_strided_lengths_are_refused():
         for paged in (False, True):
             with pytest.raises(AssertionError):
                 _cache(bad, paged)
+
+
+@pytest.mark.parametrize("many", [2 ** 31 - 1, 2 ** 31, 2 ** 32, 2 ** 32 + 5, 2 ** 63 - 1, 2 ** 64 + 1])
+def test_more_than_any_cache_holds_is_everything(native, many):
+    """A window, sinks or a number of new tokens beyond 32 bits are not taken modulo 2^32."""
+    most = 2 ** 31 - 1
+    cache, counts = _cache(), torch.zeros(5, dtype=I32)
+    ws = torch.empty(1 << 16, dtype=torch.uint8)
+    q = torch.zeros((2, 2, 3, 8, 64), dtype=BF16)
+    specvlm.window_attn(cache, q, many, many, 0.125, ws=ws)
+    specvlm.release_pages(cache, counts, window=many, n_sinks=many)
+    specvlm.release_pages(cache, counts, n_sinks=1)
+    specvlm.reserve_pages(cache, counts, many, ws=ws)
+    window, release, plain, reserve = (args for _, args in native.calls)
+    assert window[5:7] == (most, most) and release[4:6] == (most, most) and plain[4:6] == (most, 1) and reserve[4] == most
+    size = specvlm.window_attn_workspace_bytes(cache, 2, 8, 3, many, many)
+    assert size == specvlm.window_attn_workspace_bytes(cache, 2, 8, 3, most, most) > 0
+
+
+@pytest.mark.parametrize("few", [0, -1, -2 ** 31, -2 ** 32, -2 ** 32 + 5, -2 ** 40 + 1])
+def test_a_window_of_nothing_stays_one(native, few):
+    """... nor are negative ones: what is passed on is refused as it was."""
+    cache, counts = _cache(), torch.zeros(5, dtype=I32)
+    specvlm.window_attn(cache, torch.zeros((2, 2, 3, 8, 64), dtype=BF16), few, few, 0.125, ws=torch.empty(1 << 16, dtype=torch.uint8))
+    specvlm.release_pages(cache, counts, window=few, n_sinks=few)
+    specvlm.reserve_pages(cache, counts, few, ws=torch.empty(1 << 16, dtype=torch.uint8))
+    for x in native.calls[0][1][5:7] + native.calls[1][1][4:6] + native.calls[2][1][4:5]:
+        assert -2 ** 31 <= x <= 0 and (x < 0 or few == 0)
+    assert specvlm.window_attn_workspace_bytes(cache, 2, 8, 3, few, 1) == 0
