@@ -400,7 +400,6 @@ __device__ __forceinline__ void rows16_consume(const AttnParams& p, uint8_t* sme
       if (c == 0) part_lse[r] = gave_up ? __uint_as_float(kUnwritten) : lse2;
     }
     cluster_barrier();
-    bool all_used = true;
     for (int idx = rank * 128 * NG + tid; idx < rows * (D / 4); idx += n_cta * 128 * NG) {
       const int r = idx / (D / 4), c = (idx - r * (D / 4)) * 4;
       float lse[kMaxRows16Cluster];
@@ -421,10 +420,7 @@ __device__ __forceinline__ void rows16_consume(const AttnParams& p, uint8_t* sme
         lost |= unwritten(lse[k]);
         mm = fmaxf(mm, lse[k]);
       }
-      if (lost) {                                                      // a part is missing: leave the row alone
-        all_used = false;
-        continue;
-      }
+      if (lost) continue;                                              // a part is missing: leave the row alone
       float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
       for (int k = 0; k < kMaxRows16Cluster; ++k) {
@@ -441,7 +437,7 @@ __device__ __forceinline__ void rows16_consume(const AttnParams& p, uint8_t* sme
       store_bf16x4(p.out + orow * D + c, make_float4(acc.x * inv, acc.y * inv, acc.z * inv, acc.w * inv));
       if (p.lse && c == 0) p.lse[orow] = den > 0.f ? (mm + log2f(den)) * kLn2 : -INFINITY;
     }
-    cluster_barrier_after_reads(all_used);                             // nobody reads this CTA's shared memory any more
+    cluster_barrier();                                                 // nobody reads this CTA's shared memory any more
     if (gave_up && tid == 0) await_copies<STAGES>(bar_full, abort_flag);
     return;
   }

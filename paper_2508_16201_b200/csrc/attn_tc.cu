@@ -844,7 +844,6 @@ attn_tc_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__
         if (p.d_status) *p.d_status = SPECVLM_ERR_TIMEOUT;
       }
       if (n_cta > 1) cluster_barrier();                     // every role of every CTA has ended
-      bool all_used = true;
       if (n_cta > 1 && slice->first.item_tiles > 0) {
         const uint32_t part_o = smem_u32(big_ptr + C::OFF_K), part_lse = smem_u32(big_ptr + C::OFF_Q);
         const int lb = slice->first.layer * p.batch + slice->first.b, g = slice->first.g;
@@ -870,10 +869,7 @@ attn_tc_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__
             lost |= __float_as_int(flags[k]) != 0;
             mm = fmaxf(mm, lse[k]);
           }
-          if (lost) {
-            all_used = false;
-            continue;
-          }
+          if (lost) continue;
           float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
           for (int k = 0; k < kMaxTcCluster; ++k) {
@@ -895,13 +891,13 @@ attn_tc_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__
           if (p.lse && c4 == 0) p.lse[orow] = den > 0.f ? (mm + log2f(den)) * kLn2 : -INFINITY;
         }
       }
-      if (n_cta > 1) cluster_barrier_after_reads(all_used); // nobody reads this CTA's shared memory any more
+      if (n_cta > 1) cluster_barrier();                     // nobody reads this CTA's shared memory any more
     }
   }
   if constexpr (CLUSTER) {
     if (warp < 4 && p.n_cluster > 1) {                      // the other roles' part in the two barriers above
       cluster_barrier();
-      cluster_barrier_after_reads(true);
+      cluster_barrier();
     }
   }
 
