@@ -17,6 +17,7 @@
 
 #include "common.cuh"
 #include "host_util.h"
+#include "rope_turn.h"
 
 namespace specvlm {
 
@@ -96,27 +97,6 @@ __device__ __forceinline__ void turn_pairs(uint4& x, uint4& y, const uint64_t (&
       yw[w] = f2_to_bf16x2(f2_fma(b, c[w], f2_mul(a, s[w])));
     }
   }
-}
-
-// Sine and cosine of a fraction of a turn (2^32 = a whole one): reduced exactly to an eighth of a turn either way, there
-// polynomials of degree 7 and 8 (least maximum error, fitted for this file: 3.1e-9 and 5e-11), together with their rounding off
-// by at most 1.5 x 2^-24.
-__device__ __forceinline__ void turn_sincos(uint32_t turn, float& s, float& c) {
-  const uint32_t quarter = (turn + 0x20000000u) >> 30;
-  const float x = (float)(int32_t)(turn - (quarter << 30)) * 2.3283064365386963e-10f;      // 2^-32
-  const float u = x * x;
-  float sn = fmaf(u, -75.40206909179688f, 81.5925521850586f);
-  sn = fmaf(u, sn, -41.3416633605957f);
-  sn = x * fmaf(u, sn, 6.2831854820251465f);
-  float cs = fmaf(u, 59.22040557861328f, -85.44285583496094f);
-  cs = fmaf(u, cs, 64.93931579589844f);
-  cs = fmaf(u, cs, -19.739208221435547f);
-  cs = fmaf(u, cs, 1.0f);
-  const bool odd = quarter & 1u;
-  s = odd ? cs : sn;
-  c = odd ? sn : cs;
-  s = quarter & 2u ? -s : s;
-  c = (quarter + 1u) & 2u ? -c : c;
 }
 
 constexpr int kRopeThreads = 128, kRopeOneThreads = 512, kRopeOneTokens = 8, kRopeOneCtas = 8;
