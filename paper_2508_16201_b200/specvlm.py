@@ -366,20 +366,23 @@ def window_attn(kv: KvCache, q: torch.Tensor, window: int, n_sinks: int, sm_scal
                 d_status: torch.Tensor | None = None) -> torch.Tensor:
     """q, out: bf16 [n_layers][batch][n_q][n_q_heads][head_dim], lse: fp32 [n_layers][batch][n_q][n_q_heads], all contiguous; a
     query sees the last ``window`` keys up to its own and the first ``n_sinks``."""
+    bf16 = torch.bfloat16
     shape = q.shape
     L, B, NQ, Hq, D = shape
     dims = kv.dims
-    assert q.is_contiguous() and q.dtype is torch.bfloat16 and L == dims[0] and D == dims[2] and B <= kv.n_seqs
+    assert q.is_contiguous() and q.dtype is bf16 and L == dims[0] and D == dims[2] and B <= kv.n_seqs
     if out is None:
         out = torch.empty_like(q)
     else:
-        assert out.dtype is torch.bfloat16 and out.shape == shape and out.is_contiguous()
+        assert out.shape == shape and out.dtype is bf16 and out.is_contiguous()
     if lse is not None:
-        assert lse.dtype is torch.float32 and lse.shape == shape[:-1] and lse.is_contiguous()
+        assert lse.shape == (L, B, NQ, Hq) and lse.dtype is torch.float32 and lse.is_contiguous()
+    if not (0 <= window <= _I32_MAX and 0 <= n_sinks <= _I32_MAX):
+        window, n_sinks = _within_i32(window), _within_i32(n_sinks)
     if ws is None:
         ws = _ws(window_attn_workspace_bytes(kv, B, Hq, NQ, window, n_sinks), q.device)
-    rc = native().window_attn(addressof(kv.struct), q, B, Hq, NQ, _within_i32(window), _within_i32(n_sinks), float(sm_scale), out, lse,
-                              ws, ws.numel(), d_status)
+    rc = native().window_attn(addressof(kv.struct), q, B, Hq, NQ, window, n_sinks, float(sm_scale), out, lse, ws, ws.numel(),
+                              d_status)
     if rc:
         _check(rc, "specvlm_window_attn")
     return out
