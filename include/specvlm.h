@@ -26,7 +26,8 @@
  *   - `d_status` (device int32_t*, optional): a kernel that gives up a bounded wait stores
  *     SPECVLM_ERR_TIMEOUT there and returns.  A kernel that finds device-side data it would have
  *     to turn into an address out of range (a kept index, a block-table entry, a tree-path node,
- *     a sequence length) skips that access and stores SPECVLM_ERR_INVALID_ARG.  It is never
+ *     a sequence length) skips that access and stores SPECVLM_ERR_INVALID_ARG;
+ *     specvlm_reserve_pages stores SPECVLM_ERR_NO_PAGES where there are too few.  It is never
  *     written otherwise; the caller zeroes it and reads it when convenient.
  *   - Scratch memory comes from the caller: `ws` (device, 256-byte aligned) of at least the
  *     size the matching *_workspace_bytes query returns.  Its contents need not be initialised
@@ -374,6 +375,8 @@ int32_t specvlm_compact_tree_kv(const specvlm_kv_t* kv, const int32_t* path, con
  * not be mapped (specvlm_release_pages).  Rows that some query sees hold finite values.  A block-table entry outside
  * [0, n_blocks) that is needed stands for rows of zeros, and SPECVLM_ERR_INVALID_ARG is stored to d_status.
  * A query that sees no key (seq_len < n_q) gives zeros and an lse of -inf.
+ * Logits and sums are fp32.  As in the other attention calls the probabilities are rounded to bf16 for the product with V
+ * (2^-8 of each at most), the sums that divide it and the lse take them unrounded.
  * Supported: head_dim 64/128; group = n_q_heads/n_kv_heads in 1..16; batch <= 127 when group * n_q > 16; max_seq_len up
  * to 2^31 - 256.  Errors and d_status otherwise as for specvlm_verify_attn.
  */
@@ -489,13 +492,17 @@ int32_t specvlm_rope_append_kv(const specvlm_kv_t* kv, const specvlm_rope_t* rop
  * specvlm_fork_pages replaces a batch of sequences by another: row i of block_table_out and seq_lens_out goes on from
  * sequence parents[i] of kv (-1: empty).  Sequences that nobody goes on from give their pages back, and those with several
  * branches share theirs; no row is copied (specvlm_reserve_pages does that when a branch is written to).  Pages behind a
- * sequence's end are given back.  kv's table and lengths are not written, and hold no pages afterwards.
+ * sequence's end are given back.  kv's table and lengths are not written, and hold no pages afterwards.  Unlike the calls
+ * above, which leave a sequence with a length out of range alone, a fork has nowhere to leave it: it goes on as a sequence of
+ * no token and its pages are given back; so is a parent out of range a -1.  Both are reported as SPECVLM_ERR_INVALID_ARG.
  *   parents          device int32 [batch_out], batch_out <= 1024
  *   block_table_out  device int32 [batch_out][kv->max_blocks], does not overlap kv->block_table
  *   seq_lens_out     device int32 [batch_out], does not overlap kv->seq_lens
  *
  * specvlm_compact_pages moves the used pages to the front of the pool: with n used pages, the i-th used page from page n
- * on moves into the i-th free page below n (K and V, all layers and heads), and counts and table follow.
+ * on moves into the i-th free page below n (K and V, all layers and heads), and counts and table follow.  A call follows one
+ * table: batches that share a pool have their rows in one [batch][max_blocks] for it, a row of another table would go on
+ * naming the places that its pages have left.
  *   n_used_or_null   device int32 out: the number of used pages
  */
 size_t specvlm_pages_workspace_bytes(const specvlm_kv_t* kv, int32_t batch);

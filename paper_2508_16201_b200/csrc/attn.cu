@@ -156,6 +156,10 @@ struct Rows16 {
     }
     l0 = l0 * a0 + ps0;
     l1 = l1 * a1 + ps1;
+    // P goes into the product with V as bf16, the type that the tensor cores take beside V's: off by 2^-8 of each probability at most,
+    // independently of one another, so that an output, itself rounded to bf16, differs from 64 bits by 2.0e-3 to 2.3e-3 of its size
+    // instead of 1.7e-3.  The sum that divides it takes them unrounded, in fp32.  A second product for the rest of each P would double
+    // the tensor work and the conversions of a tile.
     uint32_t pa[U][4];
 #pragma unroll
     for (int u = 0; u < U; ++u) {
@@ -1092,8 +1096,9 @@ __global__ void give_up_kernel(const __grid_constant__ AttnTcParams p, int gcta,
 // are few, warps where they are many and short, tcgen05 where they are long.  Measured, tcgen05 / groups / warps, us: d = 128, 42 rows,
 // 50 items of 64 / 512 keys 6.6 / 4.5 / 5.0 and 10.4 / 9.2 / 21.2, 200 of 512 23.2 / 23.1 / 30.1, 2000 of 512 115 / 171 / 144; 24 rows, 440
 // of 64 / 256 16.2 / 10.5 / 6.2 and 25.4 / 17.8 / 16.6, 2000 of 64 / 256 61 / 41 / 30 and 74 / 70 / 72; 96 rows, 400 of 64 25.4 / 27.6 / 16.4;
-// d = 64, 36 rows, 2000 of 64 / 512 50 / 36 / 21 and 86 / 95 / 75.  The estimates below choose the fastest of the three, or one
-// within 1 % of it on average, in 594 such calls.
+// d = 64, 36 rows, 2000 of 64 / 512 50 / 36 / 21 and 86 / 95 / 75.  The estimates below choose the fastest of the three or one that
+// takes 0.9 % more on average (geometric mean; 6 % of the calls more than 5 %, none more than 25 %) in 594 calls: d = 128 with 24, 42,
+// 64, 72, 96 and 128 rows and d = 64 with 24, 36, 64, 72 and 128, 50 to 2000 items, windows of 64 to 512 keys.
 enum class RowsForm { kTc, kGroups, kWarps };
 // (kv: the positions that size the launch, of which `seen` are keys that some query sees)
 static RowsForm window_rows_form(const specvlm_kv_t* kv, int64_t seen, int32_t batch, int rows) {

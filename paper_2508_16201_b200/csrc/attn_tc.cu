@@ -538,6 +538,7 @@ attn_tc_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__
             const float nmu = m_row == -INFINITY ? 0.f : -m_row;   // a row that sees nothing yet stays at zero
             float mx4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
             ps[0] = ps[1] = 0.f;
+            // (P goes into its product as bf16, the sum takes it unrounded: Rows16::tile says why)
             tmem_ld_x16(saddr, va);
 #pragma unroll 1
             for (int cc = 0; cc < 4; ++cc) {     // 32 logits per round: four 16-byte chunks of the row
@@ -704,6 +705,7 @@ attn_tc_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__
               __syncwarp();
               if (lane == 0) mbar_arrive(bar_s_empty + 8 * grp);
             }
+            // (P goes into its product as bf16, the sum takes it unrounded: Rows16::tile says why)
 #pragma unroll
             for (int jj = 0; jj < 8; ++jj) {
               const float p0 = fast_exp2(fmaf(__uint_as_float(v[4 * jj]), p.scale_log2, nmu0));

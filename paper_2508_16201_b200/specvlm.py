@@ -579,7 +579,8 @@ def rope_append_kv(kv: KvCache, rope: Rope, q: torch.Tensor | None, new_k: torch
                    d_status: torch.Tensor | None = None) -> torch.Tensor | None:
     """q: bf16 [n_layers][batch][n_new][n_q_heads][head_dim] (None: keys only), new_k / new_v the same with the KV heads, all
     of any strides with a unit channel stride; returns the rotated queries.  kv.seq_lens is updated unless ``counted``, which
-    says that it includes the new tokens already.  positions: int32 [n_axes][batch][n_new]."""
+    says that it includes the new tokens already.  positions: int32 [n_axes][batch][n_new].  Rows of padding (behind new_lens[b])
+    are not written: they keep what q_out held, and without a q_out they are uninitialised."""
     shape = new_k.shape
     L, B, n, H, D = shape
     bf16 = torch.bfloat16
@@ -644,7 +645,7 @@ def release_pages(kv: KvCache, ref_count: torch.Tensor, window: int | None = Non
 def fork_pages(kv: KvCache, ref_count: torch.Tensor, parents: torch.Tensor, block_table_out: torch.Tensor,
                seq_lens_out: torch.Tensor, d_status: torch.Tensor | None = None) -> None:
     """Row i of block_table_out / seq_lens_out goes on from sequence parents[i] of kv (-1: empty), whose own table and lengths
-    hold no pages afterwards."""
+    hold no pages afterwards.  A length out of range counts as 0, a parent out of range as -1, and d_status says so."""
     B = _pages(kv, ref_count)
     n = parents.numel()
     assert parents.dtype == torch.int32 and parents.is_contiguous()
@@ -658,7 +659,8 @@ def fork_pages(kv: KvCache, ref_count: torch.Tensor, parents: torch.Tensor, bloc
 
 def compact_pages(kv: KvCache, ref_count: torch.Tensor, n_used: torch.Tensor | None = None, ws: torch.Tensor | None = None,
                   d_status: torch.Tensor | None = None) -> None:
-    """Moves the used pages to the front of the pool; kv's rows, kv.block_table and ref_count are updated."""
+    """Moves the used pages to the front of the pool; kv's rows, kv.block_table and ref_count are updated.  Only this table's rows
+    follow: those of all batches that share the pool have to be among them."""
     B = _pages(kv, ref_count)
     if n_used is not None:
         assert n_used.dtype == torch.int32 and n_used.numel() >= 1

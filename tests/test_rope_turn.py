@@ -1,5 +1,8 @@
 """The error that csrc/rope_turn.h states for its sine and cosine, over a sweep of the arguments of a turn on the host: fmaf and the
-fp32 products round there as they do on the device."""
+fp32 products round there as they do on the device.
+
+What the tests of the rotation allow a sine or cosine, 2^-22, follows from it: 1.73 x 2^-24 < 2^-23 here, and the angle is cut to 2^-32 of a
+turn before (1.5e-9 radians, below 2^-29)."""
 import os
 import subprocess
 
