@@ -473,7 +473,9 @@ extern "C" int32_t specvlm_rope_append_kv(const specvlm_kv_t* kv, const specvlm_
   p.axis2 = rope->n_axes > 1 ? rope->sections[0] + rope->sections[1] : rope->rot_dim;
   p.counted = counted ? 1 : 0;
   p.factor = rope->factor;
-  const int64_t tokens = (int64_t)c.n_layers * batch * n_new;
+  const int64_t sequences = (int64_t)c.n_layers * batch;
+  if (sequences > 0x3fffffff) return SPECVLM_ERR_UNSUPPORTED_SHAPE;      // (before the product, which may leave 64 bits)
+  const int64_t tokens = sequences * n_new;
   const int64_t rows = 32 / (c.head_dim / 16);
   if (tokens > 0x3fffffff || n_q_heads > 65535 || c.n_kv_heads > 65535) return SPECVLM_ERR_UNSUPPORTED_SHAPE;
   // a token's rows go to as many warps as it takes to occupy the SMs, up to a round each
