@@ -468,7 +468,7 @@ int32_t specvlm_rope_append_kv(const specvlm_kv_t* kv, const specvlm_rope_t* rop
  * how many block-table rows hold page n, 0 = free.  A table entry outside [0, n_blocks) is unmapped; these calls write -1.
  * A call covers all layers: kv describes the whole pool.  Several rows may hold a page (branches that share what came
  * before them); a row that is written to has the page to itself.  All of these calls are deterministic: free pages are
- * taken lowest first, by sequence and then position.  batch <= 1024.
+ * taken lowest first, by sequence and then position.  batch <= 1024, n_blocks < 2^30.
  *   ref_count_inout     device int32 [n_blocks]; at the start of a program zeros, with every table entry -1
  *   block_table_inout   device int32 [batch][kv->max_blocks], takes kv->block_table's place
  *   ws                  device scratch, specvlm_pages_workspace_bytes(kv, batch)

@@ -17,6 +17,7 @@ namespace specvlm {
 constexpr int kPagesMaxBatch = 1024;
 constexpr int kPlanThreads = 1024;
 constexpr int kPagesPerThread = 16;                            // counts that a planning thread holds in a round
+constexpr int32_t kPagesMost = 0x3fffffff;                     // pages of a pool: the rounds' ends stay within 32 bits
 
 struct PagesParams {
   uint4* k;
@@ -421,7 +422,7 @@ static int32_t pages_params(PagesParams& p, const specvlm_kv_t* kv, int32_t* tab
   const int32_t rc = validate_kv(&c, batch, true);
   if (rc != SPECVLM_OK) return rc;
   if (batch > kPagesMaxBatch || (int64_t)c.n_layers * c.n_kv_heads > 0x7fffffff) return SPECVLM_ERR_UNSUPPORTED_SHAPE;
-  if (c.block_tokens > (1 << 24) || (int64_t)c.max_blocks * batch > 0x3fffffff) return SPECVLM_ERR_UNSUPPORTED_SHAPE;
+  if (c.block_tokens > (1 << 24) || (int64_t)c.max_blocks * batch > 0x3fffffff || c.n_blocks > kPagesMost) return SPECVLM_ERR_UNSUPPORTED_SHAPE;
   if (needs_ws) {
     if (!ws || (reinterpret_cast<uintptr_t>(ws) & 255u)) return SPECVLM_ERR_INVALID_ARG;
     if (ws_bytes < PagesScratch(&c, batch).bytes) return SPECVLM_ERR_WORKSPACE_TOO_SMALL;
@@ -467,7 +468,8 @@ static bool overlap(const void* a, size_t a_bytes, const void* b, size_t b_bytes
 using namespace specvlm;
 
 extern "C" size_t specvlm_pages_workspace_bytes(const specvlm_kv_t* kv, int32_t batch) {
-  if (!kv || batch < 1 || batch > kPagesMaxBatch || kv->n_blocks < 1 || kv->max_blocks < 1) return 0;
+  if (!kv || batch < 1 || batch > kPagesMaxBatch || kv->n_blocks < 1 || kv->n_blocks > kPagesMost || kv->max_blocks < 1)
+    return 0;
   return PagesScratch(kv, batch).bytes;
 }
 

@@ -1,7 +1,8 @@
-"""Sizes whose product leaves 64 bits: refused by the C entries, which once divided by the number of tokens that was left of it."""
+"""Sizes that leave the integers that the entries count them in: refused."""
+import ctypes
+import os
 import subprocess
 import sys
-import os
 
 import pytest
 
@@ -22,3 +23,16 @@ def test_rope_append_refuses_more_tokens_than_it_counts(layers, batch, n_new):
 
 def _call(layers, batch, n_new):
     return _append(kv=_with(_kv, n_layers=layers), batch=batch, n_new=n_new) == specvlm.ERR_UNSUPPORTED_SHAPE
+
+
+def test_page_calls_refuse_pools_that_their_counts_leave_32_bits_in():
+    """The planning CTA goes through the pool 16 384 pages at a time, in 32 bits."""
+    L, f = specvlm.lib(), ctypes.byref
+    for pages, want in ((2 ** 30, specvlm.ERR_UNSUPPORTED_SHAPE), (2 ** 31 - 1, specvlm.ERR_UNSUPPORTED_SHAPE)):
+        kv = _with(_kv, n_blocks=pages)
+        assert L.specvlm_reserve_pages(f(kv), 0x2000, 0x6000, 2, 3, None, 0x10000, 1 << 62, None, None) == want
+        assert L.specvlm_compact_pages(f(kv), 0x2000, 0x6000, 2, None, 0x10000, 1 << 62, None, None) == want
+        assert L.specvlm_release_pages(f(kv), 0x2000, 0x6000, 2, 1, 0, None, None) == want
+        assert L.specvlm_fork_pages(f(kv), 0x6000, 2, 0x7000, 2, 0x8000, 0x9000, None, None) == want
+        assert L.specvlm_pages_workspace_bytes(f(kv), 2) == 0
+    assert L.specvlm_pages_workspace_bytes(f(_with(_kv, n_blocks=2 ** 30 - 1)), 2) > 0
